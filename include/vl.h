@@ -341,6 +341,120 @@ typedef struct {
 } vl_mask_query;
 int32_t vl_free_bases_multi(const vl_mask_query *queries, uint32_t n, uint32_t *masks, vl_stream stream);
 
+/* Token scores: what a program computes from the logits of the model that answers (Section 3.1
+ * trains it by cross entropy, Section 3.4 samples it, Section 6 proposes the verifier as its
+ * reward).  A row is the logits of one token that was or is to be emitted, over n_vocab tokens;
+ * where a token stands for a register, a window of the vocabulary is a row as well: logits points
+ * at the window's first token, ld stays the whole vocabulary's, and the words that
+ * vl_free_bases_multi writes per query are the row's mask (mask_ld 16).
+ * Of a row, with A its allowed tokens whose logit is above -infinity, m the largest logit in A, and
+ * z_t = scale * (x_t - m):
+ *   log_sum  = log( sum over A of exp(z_t) )
+ *   logprob  = z_token - log_sum; -infinity for a token outside A or not below n_vocab
+ *   entropy  = log_sum - (sum over A of z_t exp(z_t)) / (sum over A of exp(z_t))
+ *   stat     = (m, log_sum), which the gradient needs
+ *   the n_top largest logits of A, equal ones in the order of their tokens, with their logprob;
+ *   places beyond A's size get token -1 and -infinity.
+ * A row without any token in A has logprob -infinity, entropy 0 and stat (-infinity, -infinity).
+ * A row whose token is negative stands for padding: it is not read, has logprob 0, entropy 0, stat (0, 0)
+ * and no alternatives.  If an allowed logit is NaN or +infinity every number of the row is NaN and its alternatives'
+ * tokens are -1.  Sums and statistics are held in 32 bits whatever the logits' type.
+ * Results do not depend on what else runs, and a row's not on the other rows; the number of rows
+ * decides how a row's sum is split, so its last bits may differ between calls of other sizes. */
+enum { VL_F32 = 0, VL_F16 = 1, VL_BF16 = 2 };
+#define VL_MAX_VOCAB (1u << 24)
+#define VL_MAX_TOP 32u
+typedef struct {
+  const void *logits;   /* [device] row r at logits + r * ld elements, aligned to an element */
+  uint64_t ld;          /* >= n_vocab (any value for a single row) */
+  const uint32_t *mask; /* [device] bit (t & 31) of word (t >> 5) of row r, at mask + r * mask_ld: token t is
+                           allowed; bits from n_vocab on are ignored; NULL: every token is */
+  uint64_t mask_ld;     /* >= ceil(n_vocab / 32), or 0: one row of the mask serves all */
+  const int32_t *token; /* [device] [n_row] the given tokens, may be NULL */
+  uint32_t n_row;       /* >= 1, below 2^31 */
+  uint32_t n_vocab;     /* 1..VL_MAX_VOCAB */
+  uint32_t type;        /* VL_F32, VL_F16 or VL_BF16 */
+  float scale;          /* 1 / temperature: finite, > 0 */
+} vl_token_rows;
+typedef struct {        /* every pointer is [device] and may be NULL, not all of them */
+  float *logprob;       /* [n_row], needs rows->token */
+  float *entropy;       /* [n_row] */
+  float *stat;          /* [n_row][2] */
+  int32_t *top_token;   /* [n_row][n_top] */
+  float *top_logprob;   /* [n_row][n_top] */
+  uint32_t n_top;       /* 0..VL_MAX_TOP; 0 iff both of the above are NULL */
+  uint32_t reserved0;   /* must be 0 */
+} vl_token_scores;
+/* Asynchronous on `stream`: enqueues kernels only, keeps nothing between calls.  work [device]: the caller's memory for
+ * the parts of rows that are shared among workgroups, on a 16-byte boundary, of at least the bytes that
+ * vl_token_logprobs_work says for the same arguments (0 for most: work may then be NULL); its contents need not be
+ * kept or cleared, but calls that may overlap need one each, recorded ones included.
+ * Errors: VL_E_NULL, VL_E_SHAPE (a size, pitch or alignment), VL_E_RANGE (n_vocab, type, scale, n_top, reserved0);
+ * nothing is launched on error. */
+int32_t vl_token_logprobs_work(const vl_token_rows *rows, const vl_token_scores *out, uint64_t *bytes);
+int32_t vl_token_logprobs(const vl_token_rows *rows, const vl_token_scores *out, void *work, uint64_t work_bytes,
+                          vl_stream stream);
+
+/* Their gradient in the logits: with p_t = exp(z_t - log_sum), g = g_logprob[r] and e = g_entropy[r],
+ *   grad_t = scale * ( g * ((t == token) - p_t) - e * p_t * (log p_t + entropy[r]) )
+ * rounded once to the logits' type; 0 for tokens that the mask does not allow, in rows of padding and in
+ * rows without an allowed token above -infinity.  (e's term is 0 where p_t is.)  A row with NaN in its stat has NaN at its allowed
+ * tokens.  stat, and entropy with g_entropy, are what vl_token_logprobs wrote for the same rows.
+ * g_logprob [device] [n_row], needs rows->token; g_entropy [device] [n_row]; one of the two may be NULL,
+ * its values taken as 0.  grad [device]: row r at grad + r * grad_ld elements of the logits' type;
+ * what lies between rows is not written; grad may be rows->logits itself with grad_ld = ld (then
+ * the logits are overwritten), or memory apart from them.  Asynchronous on `stream`, enqueues kernels only.
+ * Errors as vl_token_logprobs. */
+int32_t vl_token_logprobs_grad(const vl_token_rows *rows, const float *stat, const float *entropy, const float *g_logprob,
+                               const float *g_entropy, void *grad, uint64_t grad_ld, vl_stream stream);
+
+/* Rewards from counted violations (Section 6: the verifier as reward), and each sample's advantage within its
+ * group, usually the K samples of one program:
+ *   reward    = extra + ok * (kinds == 0) + cons * n_cons + real * n_real + safe * n_safe
+ *   advantage = (reward - mean of its group) / (standard deviation of its group, over its size, + eps)
+ * in 64 bits, rounded once; groups of one sample or of equal rewards have advantage 0.
+ * counts [device] as vl_count_violations_multi writes them, may be NULL if extra is not (their terms are 0 then);
+ * extra [device] [n], may be NULL: any other reward, say of vl_bank_conflicts; group_off [device] [n_group + 1]: samples
+ * group_off[g] .. group_off[g + 1] - 1, non-decreasing; what lies at n or above is not touched.
+ * weights [host]; advantage, reward [device] [n], one of them may be NULL; samples of no group are not written.
+ * Asynchronous on `stream`, enqueues kernels only.
+ * Errors: VL_E_NULL, VL_E_SHAPE (n or n_group is 0, or 2^31 or more), VL_E_RANGE (a weight that is not finite, eps not finite or not > 0). */
+typedef struct { float ok, cons, real, safe; } vl_reward_weights;
+int32_t vl_group_advantages(const vl_counts *counts, const float *extra, uint32_t n, const uint32_t *group_off,
+                            uint32_t n_group, const vl_reward_weights *weights, float eps, float *reward, float *advantage,
+                            vl_stream stream);
+
+/* The clipped policy loss of sampled answers and its gradient in their tokens' log probabilities (Section 6:
+ * the verifier's feedback in training).  Sample c has the tokens start[c] .. start[c] + len[c] - 1 of the arrays below (none
+ * shared with another sample).  With a = advantage[c], d = logprob - logprob_old, q = logprob_ref - logprob:
+ *   clipped  iff a > 0 and d > log_hi, or a < 0 and d < log_lo
+ *   kl_t   = exp(q) - q - 1, 0 without logprob_ref
+ *   loss_t = -a * exp(d), or with the bound in place of d if clipped, + kl * kl_t
+ *   grad_t = weight[c] * ( -a * exp(d), or 0 if clipped, + kl * (1 - exp(q)) )
+ *   loss   = sum over c of weight[c] * sum over its tokens of loss_t; stats->kl the same of kl_t
+ * (weight: 1 / tokens of all samples, or 1 / (samples * len[c]), as the caller averages.)  d is compared with the
+ * bounds in 64 bits; sums are joined in 64 bits in an order that the sizes alone decide.  grad is written at the samples'
+ * tokens only and may be logprob itself.  Tokens at n or above are not touched, and stats->n_token leaves them out.
+ * max_len: the longest sample, as near as the host knows it: it decides the launch's shape alone.
+ * work [device]: memory of the caller as for vl_token_logprobs, at least vl_policy_loss_work bytes.
+ * Asynchronous on `stream`, enqueues kernels only.
+ * Errors: VL_E_NULL (kl != 0 without logprob_ref among them), VL_E_SHAPE (n or n_sample is 0, n_sample 2^31 or more, a pointer not aligned to its
+ * elements, work too small), VL_E_RANGE (log_lo > log_hi or one of them NaN, kl not finite); nothing is launched on error. */
+typedef struct {
+  const float *logprob, *logprob_old, *logprob_ref; /* [device] [n]; logprob_ref may be NULL */
+  uint64_t n;
+  const uint64_t *start;                            /* [device] [n_sample] */
+  const uint32_t *len;                              /* [device] [n_sample] */
+  const float *advantage, *weight;                  /* [device] [n_sample] */
+  uint32_t n_sample, max_len;
+  float log_lo, log_hi, kl;
+  uint32_t reserved0;                               /* must be 0 */
+} vl_policy_batch;
+typedef struct { float loss, kl; uint64_t n_token, n_clipped; } vl_policy_stats;
+int32_t vl_policy_loss_work(const vl_policy_batch *batch, uint64_t *bytes);
+int32_t vl_policy_loss(const vl_policy_batch *batch, float *grad, vl_policy_stats *stats, void *work, uint64_t work_bytes,
+                       vl_stream stream);
+
 const char *vl_strerror(int32_t code);
 /* hipError_t of the last failed runtime call on this thread (0 if none). */
 int32_t vl_last_hip_error(void);

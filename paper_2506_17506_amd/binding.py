@@ -62,6 +62,27 @@ class _Job(C.Structure):
                 ("ld", C.c_uint64), ("out", C.c_void_p)]
 
 
+class _TokenRows(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("ld", C.c_uint64), ("mask", C.c_void_p), ("mask_ld", C.c_uint64), ("token", C.c_void_p),
+                ("n_row", C.c_uint32), ("n_vocab", C.c_uint32), ("type", C.c_uint32), ("scale", C.c_float)]
+
+
+class _TokenScores(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("logprob", "entropy", "stat", "top_token", "top_logprob")] + \
+               [("n_top", C.c_uint32), ("reserved0", C.c_uint32)]
+
+
+class _RewardWeights(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("ok", "cons", "real", "safe")]
+
+
+class _PolicyBatch(C.Structure):
+    _fields_ = [("logprob", C.c_void_p), ("logprob_old", C.c_void_p), ("logprob_ref", C.c_void_p), ("n", C.c_uint64),
+                ("start", C.c_void_p), ("len", C.c_void_p), ("advantage", C.c_void_p), ("weight", C.c_void_p),
+                ("n_sample", C.c_uint32), ("max_len", C.c_uint32), ("log_lo", C.c_float), ("log_hi", C.c_float),
+                ("kl", C.c_float), ("reserved0", C.c_uint32)]
+
+
 _lib = None
 
 
@@ -110,6 +131,19 @@ def load():
         L.vl_bank_conflicts.argtypes = [C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p]
         L.vl_free_bases_multi.restype = C.c_int32
         L.vl_free_bases_multi.argtypes = [C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p]
+        L.vl_token_logprobs_work.restype = C.c_int32
+        L.vl_token_logprobs_work.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
+        L.vl_token_logprobs.restype = C.c_int32
+        L.vl_token_logprobs.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
+        L.vl_token_logprobs_grad.restype = C.c_int32
+        L.vl_token_logprobs_grad.argtypes = [C.c_void_p] * 6 + [C.c_uint64, C.c_void_p]
+        L.vl_group_advantages.restype = C.c_int32
+        L.vl_group_advantages.argtypes = [C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_uint32, C.c_void_p, C.c_float,
+                                          C.c_void_p, C.c_void_p, C.c_void_p]
+        L.vl_policy_loss_work.restype = C.c_int32
+        L.vl_policy_loss_work.argtypes = [C.c_void_p, C.c_void_p]
+        L.vl_policy_loss.restype = C.c_int32
+        L.vl_policy_loss.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
         L.vl_strerror.restype = C.c_char_p
         L.vl_strerror.argtypes = [C.c_int32]
         L.vl_last_hip_error.restype = C.c_int32
@@ -337,6 +371,196 @@ def vl_free_bases_multi(queries, masks, stream=None) -> None:
     rc = load().vl_free_bases_multi(arr, len(arr), C.c_void_p(_dev_ptr(masks)), _stream_ptr(stream))
     if rc != 0:
         raise VlError(rc, "vl_free_bases_multi")
+
+
+# ---- token scores and the policy loss: torch tensors on the current device, from which the sizes are taken
+
+VL_F32, VL_F16, VL_BF16 = 0, 1, 2
+VL_MAX_VOCAB, VL_MAX_TOP = 1 << 24, 32
+_TYPE = {"torch.float32": VL_F32, "torch.float16": VL_F16, "torch.bfloat16": VL_BF16}
+_WORDS = ("torch.int32", "torch.uint32")
+POLICY_STATS_DTYPE = np.dtype([("loss", "<f4"), ("kl", "<f4"), ("n_token", "<u8"), ("n_clipped", "<u8")])   # vl_policy_stats
+
+
+def _need(what, ok, code=-2):
+    if not ok:
+        raise VlError(code, what)
+
+
+def _tensor(what, x, dtypes, shape=None, nullable=True):
+    """The pointer of a contiguous tensor of one of the types (and of that shape), None for None."""
+    if x is None:
+        _need(what, nullable, -1)
+        return None
+    _here(what, x)
+    _need(what, str(x.dtype) in dtypes, -3)
+    _need(what, x.is_contiguous() and (shape is None or tuple(x.shape) == shape))
+    return x.data_ptr()
+
+
+_current_device = None
+
+
+def _here(what, x):
+    """tensors of another device than the current one, and of the host, are refused"""
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = torch.cuda.current_device
+    d = x.device
+    _need(what, d.type == "cuda" and d.index == _current_device(), -7)
+
+
+def _token_rows(what, logits, token, mask, scale):
+    _here(what, logits)
+    _need(what, str(logits.dtype) in _TYPE, -3)
+    _need(what, logits.dim() == 2 and (logits.shape[1] <= 1 or logits.stride(1) == 1))
+    n, v = logits.shape
+    a = _TokenRows(logits.data_ptr(), logits.stride(0), None, 0, None, n, v, _TYPE[str(logits.dtype)], scale)
+    if mask is not None:
+        _here(what, mask)
+        _need(what, str(mask.dtype) in _WORDS, -3)
+        shared = mask.dim() == 1
+        _need(what, mask.dim() in (1, 2) and mask.stride(-1) == 1 and mask.shape[-1] * 32 >= v and (shared or mask.shape[0] == n))
+        a.mask, a.mask_ld = mask.data_ptr(), 0 if shared or n == 1 else mask.stride(0)
+    a.token = _tensor(what, token, ("torch.int32",), (n,))
+    return a
+
+
+def _work(n_bytes, stream, device):
+    """memory for one call on the stream it runs on"""
+    import torch
+    if stream is None:
+        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(getattr(stream, "value", stream) or 0), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+
+
+def _work_bytes(what, call, work, stream, device, *args):
+    """(pointer, bytes, the tensor) of what `call` says the call needs: `work` or memory of the call's own"""
+    need = C.c_uint64()
+    rc = call(*args, C.byref(need))
+    if rc != 0:
+        raise VlError(rc, what)
+    if work is not None:
+        _here(what, work)
+        _need(what, work.is_contiguous())
+    elif need.value:
+        work = _work(need.value, stream, device)
+    return (None, 0, None) if work is None else (work.data_ptr(), work.numel() * work.element_size(), work)
+
+
+def vl_token_logprobs_work(logits, token=None, mask=None, scale=1.0, logprob=None, entropy=None, stat=None, top_token=None,
+                           top_logprob=None) -> int:
+    """Bytes of work that vl_token_logprobs needs for the same arguments."""
+    a, o = _token_scores(logits, token, mask, scale, logprob, entropy, stat, top_token, top_logprob)
+    return _work_bytes_only("vl_token_logprobs_work", load().vl_token_logprobs_work, C.byref(a), C.byref(o))
+
+
+def _work_bytes_only(what, call, *args):
+    need = C.c_uint64()
+    rc = call(*args, C.byref(need))
+    if rc != 0:
+        raise VlError(rc, what)
+    return need.value
+
+
+def _token_scores(logits, token, mask, scale, logprob, entropy, stat, top_token, top_logprob):
+    what = "vl_token_logprobs"
+    a = _token_rows(what, logits, token, mask, scale)
+    n, f = a.n_row, ("torch.float32",)
+    some = top_token if top_token is not None else top_logprob
+    _need(what, some is None or some.dim() == 2)
+    k = 0 if some is None else some.shape[1]
+    o = _TokenScores(_tensor(what, logprob, f, (n,)), _tensor(what, entropy, f, (n,)), _tensor(what, stat, f, (n, 2)),
+                     _tensor(what, top_token, ("torch.int32",), (n, k)), _tensor(what, top_logprob, f, (n, k)), k, 0)
+    return a, o
+
+
+def vl_token_logprobs(logits, token=None, mask=None, scale=1.0, logprob=None, entropy=None, stat=None, top_token=None,
+                      top_logprob=None, work=None, stream=None) -> None:
+    """logits [n_row, n_vocab] in float32, float16 or bfloat16, rows of any pitch (a window of the columns of wider rows is
+    one); token int32 [n_row]; mask int32 words [n_row, words] or [words] for all rows.  Written, those that are given:
+    logprob, entropy float32 [n_row], stat float32 [n_row, 2], top_token int32 and top_logprob float32 [n_row, n_top].
+    work: memory of vl_token_logprobs_work bytes, allocated on the call's stream if not given."""
+    a, o = _token_scores(logits, token, mask, scale, logprob, entropy, stat, top_token, top_logprob)
+    L = load()
+    p, n_bytes, keep = _work_bytes("vl_token_logprobs", L.vl_token_logprobs_work, work, stream, logits.device, C.byref(a), C.byref(o))
+    rc = L.vl_token_logprobs(C.byref(a), C.byref(o), p, n_bytes, _stream_ptr(stream))
+    if rc != 0:
+        raise VlError(rc, "vl_token_logprobs")
+
+
+def vl_token_logprobs_grad(logits, stat, grad, token=None, mask=None, scale=1.0, entropy=None, g_logprob=None, g_entropy=None,
+                           stream=None) -> None:
+    """grad [n_row, n_vocab] of the logits' type and any pitch, or logits itself; stat and entropy as vl_token_logprobs wrote
+    them for the same rows; g_logprob, g_entropy float32 [n_row]."""
+    what = "vl_token_logprobs_grad"
+    a = _token_rows(what, logits, token, mask, scale)
+    _here(what, grad)
+    _need(what, grad.dtype == logits.dtype, -3)
+    _need(what, grad.shape == logits.shape and (grad.shape[1] <= 1 or grad.stride(1) == 1))
+    f, n = ("torch.float32",), (a.n_row,)
+    rc = load().vl_token_logprobs_grad(C.byref(a), _tensor(what, stat, f, (a.n_row, 2)), _tensor(what, entropy, f, n),
+                                       _tensor(what, g_logprob, f, n), _tensor(what, g_entropy, f, n), grad.data_ptr(),
+                                       grad.stride(0), _stream_ptr(stream))
+    if rc != 0:
+        raise VlError(rc, what)
+
+
+def vl_group_advantages(counts, group_off, weights, eps, advantage, reward=None, extra=None, stream=None) -> None:
+    """counts: the records vl_count_violations_multi wrote (int32 [n, 8] or 32 n bytes) or None; group_off int32 [n_group + 1];
+    weights: (ok, cons, real, safe); advantage, reward, extra float32 [n]."""
+    what = "vl_group_advantages"
+    f = ("torch.float32",)
+    some = next((x for x in (advantage, reward, extra) if x is not None), None)
+    _need(what, some is not None, -1)
+    n = some.numel()
+    p = _tensor(what, counts, ("torch.int32", "torch.uint32", "torch.uint8"))
+    _need(what, counts is None or counts.numel() * counts.element_size() == 32 * n)
+    off = _tensor(what, group_off, _WORDS, nullable=False)
+    w = _RewardWeights(*weights)
+    rc = load().vl_group_advantages(p, _tensor(what, extra, f, (n,)), n, off, max(0, group_off.numel() - 1), C.byref(w), eps,
+                                    _tensor(what, reward, f, (n,)), _tensor(what, advantage, f, (n,)), _stream_ptr(stream))
+    if rc != 0:
+        raise VlError(rc, what)
+
+
+def _policy_batch(logprob, logprob_old, start, length, advantage, weight, log_lo, log_hi, logprob_ref, kl, max_len):
+    what = "vl_policy_loss"
+    f = ("torch.float32",)
+    _need(what, start is not None and logprob is not None, -1)
+    n, m = tuple(logprob.shape), (start.numel(),)
+    if max_len is None:   # the samples' mean, at most: a launch's shape, not a bound
+        max_len = min(0xFFFFFFFF, logprob.numel() // max(1, m[0]) + 1)
+    return _PolicyBatch(_tensor(what, logprob, f), _tensor(what, logprob_old, f, n, False), _tensor(what, logprob_ref, f, n),
+                        logprob.numel(), _tensor(what, start, ("torch.int64", "torch.uint64"), m), _tensor(what, length, _WORDS, m, False),
+                        _tensor(what, advantage, f, m, False), _tensor(what, weight, f, m, False), m[0], max_len, log_lo, log_hi, kl, 0)
+
+
+def vl_policy_loss_work(logprob, logprob_old, start, length, advantage, weight, log_lo, log_hi, logprob_ref=None, kl=0.0,
+                        max_len=None) -> int:
+    """Bytes of work that vl_policy_loss needs for the same arguments."""
+    b = _policy_batch(logprob, logprob_old, start, length, advantage, weight, log_lo, log_hi, logprob_ref, kl, max_len)
+    return _work_bytes_only("vl_policy_loss_work", load().vl_policy_loss_work, C.byref(b))
+
+
+def vl_policy_loss(logprob, logprob_old, start, length, advantage, weight, grad, stats, log_lo, log_hi, logprob_ref=None, kl=0.0,
+                   max_len=None, work=None, stream=None) -> None:
+    """logprob, logprob_old, logprob_ref, grad: float32 of one shape; start int64, length int32, advantage, weight float32
+    [n_sample]; stats: device buffer of one POLICY_STATS_DTYPE record (24 bytes); max_len: the longest sample if known."""
+    what = "vl_policy_loss"
+    b = _policy_batch(logprob, logprob_old, start, length, advantage, weight, log_lo, log_hi, logprob_ref, kl, max_len)
+    p_grad = _tensor(what, grad, ("torch.float32",), tuple(logprob.shape), False)
+    p_stats = _tensor(what, stats, ("torch.uint8", "torch.int32", "torch.int64"), nullable=False)
+    _need(what, stats.numel() * stats.element_size() >= 24)
+    L = load()
+    p, n_bytes, keep = _work_bytes(what, L.vl_policy_loss_work, work, stream, logprob.device, C.byref(b))
+    rc = L.vl_policy_loss(C.byref(b), p_grad, p_stats, p, n_bytes, _stream_ptr(stream))
+    if rc != 0:
+        raise VlError(rc, what)
 
 
 def _dev_ptr(x) -> int:

@@ -4,7 +4,7 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = ["vl_mir.hip", "vl_liveness.hip", "vl_verify.hip", "vl_mask.hip", "vl_count.hip", "vl_score.hip"]
+SOURCES = ["vl_mir.hip", "vl_liveness.hip", "vl_verify.hip", "vl_mask.hip", "vl_count.hip", "vl_score.hip", "vl_token.hip", "vl_policy.hip"]
 BENCH_SOURCES = ["vl_probe.hip"]   # measurement hooks of the benchmark (include/vl_bench.h), a library of their own
 LIB = os.path.join(HERE, "libvl.so")
 BENCH_LIB = os.path.join(HERE, "libvlbench.so")
