@@ -364,6 +364,7 @@ int32_t vl_free_bases_multi(const vl_mask_query *queries, uint32_t n, uint32_t *
 enum { VL_F32 = 0, VL_F16 = 1, VL_BF16 = 2 };
 #define VL_MAX_VOCAB (1u << 24)
 #define VL_MAX_TOP 32u
+#define VL_MIN_SCALE 0x1p-64f
 typedef struct {
   const void *logits;   /* [device] row r at logits + r * ld elements, aligned to an element */
   uint64_t ld;          /* >= n_vocab (any value for a single row) */
@@ -374,7 +375,7 @@ typedef struct {
   uint32_t n_row;       /* >= 1, below 2^31 */
   uint32_t n_vocab;     /* 1..VL_MAX_VOCAB */
   uint32_t type;        /* VL_F32, VL_F16 or VL_BF16 */
-  float scale;          /* 1 / temperature: finite, > 0 */
+  float scale;          /* 1 / temperature: VL_MIN_SCALE .. 1 / VL_MIN_SCALE */
 } vl_token_rows;
 typedef struct {        /* every pointer is [device] and may be NULL, not all of them */
   float *logprob;       /* [n_row], needs rows->token */

@@ -1,5 +1,20 @@
 // Token scores: log probabilities of given tokens, entropy and the largest logits of each row
 // over the tokens its mask leaves, and the gradient of the first two in the logits.
+//
+// A row is read once.  Its logits are taken in chunks of 16 bytes, wherever the row starts (the
+// card reads and writes 16 bytes at any address; a chunk that the row's end cuts is taken an element at a time).
+// A lane holds the largest logit m of its chunks so far, the sum S of exp(z) for z = scale (x - m), and the sum Y of
+// z exp(z): when m grows by d, S is scaled by exp(-d) and Y becomes exp(-d) (Y - d S).  All terms of S have one sign, and
+// all of Y, so log S - Y / S, the entropy, loses nothing.  Lanes, wavefronts and parts of rows are joined the
+// same way.  z is kept in powers of two (scale * log2 e in one factor), for the card's exp2.
+//
+// The n best of a row cost the loop next to nothing: a lane also keeps which of its chunks its m came from.  The n lanes
+// with the best (m, chunk) hold all of the row's n best: any other lane's best is below n
+// larger ones.  Their chunks, n / 256 of the row, are read again, and what is not below the worst of those n maxima is put
+// into a sorted list that a wavefront's lanes hold, an entry each.
+#include <algorithm>
+#include <type_traits>
+
 #include "vl_dev.h"
 
 using namespace vl;
@@ -7,127 +22,642 @@ using namespace vl;
 namespace {
 
 constexpr float kNoLogit = -__builtin_huge_valf();
+constexpr float kLeast = -3.402823466e38f;   // stands for m where there is none, so that no difference is of two infinities
+constexpr float kFar = -1000.0f;             // (powers of two) exp2 gives 0 long before; keeps 0 * infinity out of Y
+constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.69314718055994f;
 
 struct Rows {
   const uint8_t VL_GLOBAL *logits;
   uint64_t ld;                         // in bytes
-  const uint32_t VL_GLOBAL *mask;
-  uint64_t mask_ld;
+  const uint8_t VL_GLOBAL *mask;
+  uint64_t mask_ld;                    // in bytes
   const int32_t VL_GLOBAL *token;
   uint32_t n_row, n_vocab;
-  float scale;
+  float scale, scale2;                 // scale2 = scale * log2 e
+};
+struct Scores {
+  float VL_GLOBAL *logprob, *entropy, *stat, *top_logprob;
+  int32_t VL_GLOBAL *top_token;
+  uint32_t n_top;
 };
 
-struct F32 { typedef float type; static __device__ float wide(float x) { return x; } static __device__ float narrow(float x) { return x; } };
-struct F16 { typedef _Float16 type; static __device__ float wide(_Float16 x) { return (float)x; } static __device__ _Float16 narrow(float x) { return (_Float16)x; } };
-struct BF16 { typedef __bf16 type; static __device__ float wide(__bf16 x) { return (float)x; } static __device__ __bf16 narrow(float x) { return (__bf16)x; } };
+__device__ inline float as_float(uint32_t x) { return __builtin_bit_cast(float, x); }
+__device__ inline uint32_t as_word(float x) { return __builtin_bit_cast(uint32_t, x); }
+
+struct F32 {
+  typedef float type;
+  typedef u32x4 chunk __attribute__((aligned(4)));
+  static constexpr uint32_t kElems = 4;
+  static __device__ inline float wide(float x) { return x; }
+  static __device__ inline float narrow(float x) { return x; }
+  static __device__ inline void unpack(u32x4 w, float *x) {
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) x[j] = as_float(w[j]);
+  }
+  static __device__ inline u32x4 pack(const float *x) {
+    u32x4 w;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) w[j] = as_word(x[j]);
+    return w;
+  }
+};
+struct F16 {
+  typedef _Float16 type;
+  typedef _Float16 pair __attribute__((ext_vector_type(2)));
+  typedef u32x4 chunk __attribute__((aligned(2)));
+  static constexpr uint32_t kElems = 8;
+  static __device__ inline float wide(_Float16 x) { return (float)x; }
+  static __device__ inline _Float16 narrow(float x) { return (_Float16)x; }
+  static __device__ inline void unpack(u32x4 w, float *x) {
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+      const uint32_t both = w[j];   // (a bit cast of a vector's element itself takes the first one)
+      const pair p = __builtin_bit_cast(pair, both);
+      x[2 * j] = (float)p.x;
+      x[2 * j + 1] = (float)p.y;
+    }
+  }
+  static __device__ inline u32x4 pack(const float *x) {
+    u32x4 w;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) w[j] = __builtin_bit_cast(uint32_t, pair{(_Float16)x[2 * j], (_Float16)x[2 * j + 1]});
+    return w;
+  }
+};
+struct BF16 {
+  typedef __bf16 type;
+  typedef __bf16 pair __attribute__((ext_vector_type(2)));
+  typedef u32x4 chunk __attribute__((aligned(2)));
+  static constexpr uint32_t kElems = 8;
+  static __device__ inline float wide(__bf16 x) { return (float)x; }
+  static __device__ inline __bf16 narrow(float x) { return (__bf16)x; }
+  static __device__ inline void unpack(u32x4 w, float *x) {
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+      x[2 * j] = as_float(w[j] << 16);
+      x[2 * j + 1] = as_float(w[j] & 0xFFFF0000u);
+    }
+  }
+  static __device__ inline u32x4 pack(const float *x) {
+    u32x4 w;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) w[j] = __builtin_bit_cast(uint32_t, pair{(__bf16)x[2 * j], (__bf16)x[2 * j + 1]});
+    return w;
+  }
+};
+
+constexpr uint32_t kThreads = 256, kWaves = kThreads / 64;
 
 template <class T>
-__device__ inline float logit(const Rows &a, uint32_t r, uint32_t t) {
-  if (a.mask && !((a.mask[(uint64_t)r * a.mask_ld + (t >> 5)] >> (t & 31u)) & 1u)) return kNoLogit;
-  return T::wide(((const typename T::type VL_GLOBAL *)(a.logits + (uint64_t)r * a.ld))[t]);
+__device__ inline u32x4 load_chunk(const uint8_t VL_GLOBAL *row, uint32_t c) {
+  return *(const typename T::chunk VL_GLOBAL *)(row + (uint64_t)c * 16);
 }
 
-constexpr uint32_t kThreads = 256;
+// the logits that the mask does not allow become -infinity (bit j of `bits`: logit j is allowed)
+template <class T>
+__device__ inline void keep_allowed(float *x, uint32_t bits) {
+#pragma unroll
+  for (uint32_t j = 0; j < T::kElems; ++j) {
+    const uint32_t keep = (uint32_t)((int32_t)(bits << (31 - j)) >> 31);
+    x[j] = as_float((as_word(x[j]) & keep) | (0xFF800000u & ~keep));
+  }
+}
+template <class T>
+__device__ inline uint32_t mask_bits(const uint8_t VL_GLOBAL *mask, uint32_t c) {   // of chunk c, in the low bits
+  if (T::kElems == 8) return mask[c];
+  return mask[c >> 1] >> ((c & 1) * 4);
+}
 
-struct Best { float x; uint32_t t; };   // a logit and its token; better: larger, or equal and of a lower token
-__device__ inline bool better(Best a, Best b) { return a.x > b.x || (a.x == b.x && a.t < b.t); }
+// chunk c of a row of n logits, of which the row's end may cut some off: those are -infinity
+template <class T>
+__device__ inline void load_any(const Rows &a, const uint8_t VL_GLOBAL *row, const uint8_t VL_GLOBAL *mask, uint32_t c, float *x) {
+  const uint32_t from = c * T::kElems;
+  if (from + T::kElems <= a.n_vocab) {
+    T::unpack(load_chunk<T>(row, c), x);
+  } else {
+#pragma unroll
+    for (uint32_t j = 0; j < T::kElems; ++j)
+      x[j] = from + j < a.n_vocab ? T::wide(((const typename T::type VL_GLOBAL *)row)[from + j]) : kNoLogit;
+  }
+  if (mask) keep_allowed<T>(x, from < a.n_vocab ? mask_bits<T>(mask, c) : 0u);
+}
 
-template <class F, class V>
-__device__ V block_reduce(V v, V *room, F join) {
-  room[threadIdx.x] = v;
+// ---- over a wavefront: rows of 16 lanes, then across rows; the result stands in lane 63
+template <class F>
+__device__ inline float wave_fold(float x, float none, F f) {
+  auto step = [&](auto ctrl, auto rows) {
+    const int y = __builtin_amdgcn_update_dpp((int)as_word(none), (int)as_word(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    x = f(x, as_float((uint32_t)y));
+  };
+  step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr:1, 2, 4, 8
+  step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+  step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+  step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+  step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast:15 into rows 1 and 3
+  step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast:31 into rows 2 and 3
+  return as_float((uint32_t)__builtin_amdgcn_readlane((int)as_word(x), 63));
+}
+__device__ inline float wave_max(float x) { return wave_fold(x, kNoLogit, [](float u, float v) { return fmaxf(u, v); }); }
+__device__ inline float wave_sum(float x) { return wave_fold(x, 0.0f, [](float u, float v) { return u + v; }); }
+
+// ---- a row's sums so far
+struct Sums { float m, s, y; };
+__device__ inline float ref_of(float m) { return fmaxf(m, kLeast); }
+// `from` seen from the larger maximum `m`
+__device__ inline Sums rebase(Sums from, float m, float scale2) {
+  const float d = fmaxf((ref_of(from.m) - ref_of(m)) * scale2, kFar), f = __builtin_amdgcn_exp2f(d);
+  return Sums{m, from.s * f, f * (from.y + d * from.s)};
+}
+
+// ---- the best: logits with their tokens as one number, larger = better (a larger logit, or an equal one of a lower token)
+__device__ inline uint32_t ordered(float x) {
+  const uint32_t b = as_word(x + 0.0f);   // (one zero)
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ inline float unordered(uint32_t u) { return as_float(u ^ ((u >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
+__device__ inline uint64_t key_of(uint32_t value, uint32_t place) { return ((uint64_t)value << 32) | (uint32_t)~place; }
+__device__ inline uint64_t lane_key(uint64_t k, uint32_t lane) {
+  return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
+}
+
+// A sorted list, entry i in lane i, 0 where there is none; `worst` is entry n - 1.
+struct List {
+  uint64_t key = 0, worst = 0;
+  __device__ inline void insert(uint64_t k, uint32_t n) {   // (k the same in all lanes)
+    if (k <= worst) return;
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint32_t at = __popcll(__ballot(key > k));
+    // entries from `at` on move up one lane
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)key, 0x138, 0xf, 0xf, false);   // wave_shr:1
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(key >> 32), 0x138, 0xf, 0xf, false);
+    key = lane < at ? key : lane == at ? k : ((uint64_t)hi << 32) | lo;
+    worst = lane_key(key, n - 1);
+  }
+  // what the lanes where `ask` is set hold
+  __device__ inline void insert_lanes(uint64_t k, bool ask, uint32_t n) {
+    for (uint64_t todo = __ballot(ask); todo; todo &= todo - 1) insert(lane_key(k, (uint32_t)__builtin_ctzll(todo)), n);
+  }
+};
+
+// The n-th largest of the keys that a wavefront's lanes hold, kEach per lane, bit by bit from the top, until no more
+// than n are at or above it; 1 if there are fewer than n (0: no key).  All keys but 0 differ.
+template <uint32_t kEach>
+__device__ inline uint64_t nth_key(const uint64_t *k, uint32_t n) {
+  uint64_t least = 0;
+  for (int32_t bit = 63; bit >= 0; --bit) {
+    const uint64_t attempt = least | (1ull << bit);
+    uint32_t count = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) count += __popcll(__ballot(k[i] >= attempt));
+    if (count < n) continue;
+    least = attempt;
+    if (count == n) break;
+  }
+  return least ? least : 1ull;
+}
+
+// A chunk's logits that can be among the n best go into the list: `least` is a lane's (value, chunk) that n lanes' best reach
+template <class T>
+__device__ inline void list_chunk(List &list, const float *x, uint32_t c, uint64_t least, uint32_t n) {
+  const uint32_t value = (uint32_t)(least >> 32) + (c <= (uint32_t)~least ? 0u : 1u);
+#pragma unroll
+  for (uint32_t j = 0; j < T::kElems; ++j) {
+    const uint32_t u = ordered(x[j]);
+    list.insert_lanes(key_of(u, c * T::kElems + j), x[j] != kNoLogit && u >= value, n);
+  }
+}
+
+// ---- what a row's results are made of
+struct Final { float m, s, log_sum, scale; bool bad; };
+__device__ inline float logprob_of(const Final &f, float x) {
+  return f.bad ? f.s : x == kNoLogit ? kNoLogit : (x - ref_of(f.m)) * f.scale - f.log_sum;
+}
+__device__ inline Final finish(const Rows &a, const Scores &out, uint32_t r, Sums sums, float x, bool write) {
+  const Final f = {sums.m, sums.s, logf(sums.s), a.scale, sums.s != sums.s};
+  if (write) {
+    if (out.logprob) out.logprob[r] = logprob_of(f, x);
+    if (out.entropy) out.entropy[r] = f.s == 0.0f ? 0.0f : f.log_sum - kLn2 * sums.y / f.s;
+    if (out.stat) {
+      out.stat[2ull * r] = f.bad ? f.s : f.m;
+      out.stat[2ull * r + 1] = f.log_sum;
+    }
+  }
+  return f;
+}
+__device__ inline void write_top(const Scores &out, uint32_t r, uint32_t k, uint64_t key, const Final &f) {
+  const uint64_t at = (uint64_t)r * out.n_top + k;
+  if (out.top_token) out.top_token[at] = key && !f.bad ? (int32_t)~(uint32_t)key : -1;
+  if (out.top_logprob) out.top_logprob[at] = f.bad ? f.s : key ? logprob_of(f, unordered((uint32_t)(key >> 32))) : kNoLogit;
+}
+// a row of padding; `lane` of 64 or more
+__device__ inline void write_padding(const Scores &out, uint32_t r, uint32_t lane) {
+  if (lane == 0) {
+    if (out.logprob) out.logprob[r] = 0.0f;
+    if (out.entropy) out.entropy[r] = 0.0f;
+    if (out.stat) out.stat[2ull * r] = out.stat[2ull * r + 1] = 0.0f;
+  }
+  if (lane < out.n_top) write_top(out, r, lane, 0, Final{0, 0, 0, 0, false});
+}
+// the given token's logit, -infinity if there is none
+template <class T>
+__device__ inline float given_logit(const Rows &a, uint32_t r, int32_t token) {
+  if (!a.token || (uint32_t)token >= a.n_vocab) return kNoLogit;
+  if (a.mask && !((a.mask[(uint64_t)r * a.mask_ld + ((uint32_t)token >> 3)] >> (token & 7)) & 1)) return kNoLogit;
+  return T::wide(((const typename T::type VL_GLOBAL *)(a.logits + (uint64_t)r * a.ld))[token]);
+}
+
+// Short rows: a wavefront per row, kChunks chunks per lane, all in registers.
+template <class T, uint32_t kChunks>
+__global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
+  const uint32_t lane = threadIdx.x & 63u;
+  for (uint32_t r = blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < a.n_row; r += gridDim.x * kWaves) {
+    const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
+    const uint8_t VL_GLOBAL *mask = a.mask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
+    const int32_t token = a.token ? a.token[r] : 0;
+    if (token < 0) {
+      write_padding(out, r, lane);
+      continue;
+    }
+    float x[kChunks][T::kElems];
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i) load_any<T>(a, row, mask, lane + 64 * i, x[i]);
+    const float given = given_logit<T>(a, r, token);
+    float m = kNoLogit;
+    uint32_t place = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i) {
+      float b = x[i][0];
+#pragma unroll
+      for (uint32_t j = 1; j < T::kElems; ++j) b = fmaxf(b, x[i][j]);
+      if (b > m) place = lane + 64 * i;
+      m = fmaxf(m, b);
+    }
+    Sums sums = {wave_max(m), 0.0f, 0.0f};
+    const float ref = ref_of(sums.m);
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i)
+#pragma unroll
+      for (uint32_t j = 0; j < T::kElems; ++j) {
+        const float z = (x[i][j] - ref) * a.scale2, e = __builtin_amdgcn_exp2f(z);
+        sums.s += e;
+        sums.y += e * fmaxf(z, kFar);
+      }
+    sums.s = wave_sum(sums.s);
+    if (out.entropy) sums.y = wave_sum(sums.y);
+    const Final f = finish(a, out, r, sums, given, lane == 0);
+    if (out.n_top) {
+      const uint64_t key = m == kNoLogit ? 0ull : key_of(ordered(m), place);
+      const uint64_t least = nth_key<1>(&key, out.n_top);
+      List list;
+#pragma unroll
+      for (uint32_t i = 0; i < kChunks; ++i) list_chunk<T>(list, x[i], lane + 64 * i, least, out.n_top);
+      if (lane < out.n_top) write_top(out, r, lane, list.key, f);
+    }
+  }
+}
+
+// What a part of a row leaves for the join: its sums and n_top keys, best first.
+typedef float Part __attribute__((ext_vector_type(4)));
+
+struct Shared {
+  Sums sums[kWaves];
+  uint64_t key[kThreads];
+  uint64_t list[kWaves][VL_MAX_TOP];
+  uint64_t least;
+  uint32_t n_hot, hot[VL_MAX_TOP];
+};
+
+// the wavefronts' lists as one, best first: entry k of it in thread k < n_top; by rank, since all keys differ
+__device__ inline uint64_t join_lists(Shared &sh, const List &list, uint32_t n) {
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+  if (lane < VL_MAX_TOP) sh.list[wave][lane] = lane < n ? list.key : 0ull;
   __syncthreads();
-  for (uint32_t d = kThreads / 2; d; d /= 2) {
-    if (threadIdx.x < d) room[threadIdx.x] = join(room[threadIdx.x], room[threadIdx.x + d]);
+  uint64_t *out = sh.key;   // (done with by now)
+  if (threadIdx.x < kWaves * VL_MAX_TOP) {
+    const uint64_t mine = (&sh.list[0][0])[threadIdx.x];
+    uint32_t rank = 0, some = 0;
+    for (uint32_t w = 0; w < kWaves; ++w)
+      for (uint32_t k = 0; k < n; ++k) {
+        const uint64_t other = sh.list[w][k];
+        rank += other > mine;
+        some += other != 0;
+      }
+    if (mine && rank < n) out[rank] = mine;
+    if (threadIdx.x < n && threadIdx.x >= some) out[threadIdx.x] = 0;
+  }
+  __syncthreads();
+  return threadIdx.x < n ? out[threadIdx.x] : 0ull;
+}
+
+__device__ inline Sums join_sums(Shared &sh, Sums mine, float scale2) {
+  const float wm = wave_max(mine.m);
+  mine = rebase(mine, wm, scale2);
+  mine.s = wave_sum(mine.s);
+  mine.y = wave_sum(mine.y);
+  if ((threadIdx.x & 63u) == 0) sh.sums[threadIdx.x >> 6] = mine;
+  __syncthreads();
+  float m = sh.sums[0].m;
+  for (uint32_t w = 1; w < kWaves; ++w) m = fmaxf(m, sh.sums[w].m);
+  Sums all = {m, 0.0f, 0.0f};
+  for (uint32_t w = 0; w < kWaves; ++w) {
+    const Sums p = rebase(sh.sums[w], m, scale2);
+    all.s += p.s;
+    all.y += p.y;
+  }
+  return all;
+}
+
+constexpr uint32_t kBatch = 4;   // chunks of a lane on their way at once
+
+// Long rows: a workgroup per row or part of a row.  Thread t takes the part's chunks t, t + 256, t + 512, ...
+template <class T, bool kMask, bool kEntropy>
+__global__ __launch_bounds__(kThreads) void k_scores_long(Rows a, Scores out, uint32_t part_chunks, Part VL_GLOBAL *parts, uint64_t VL_GLOBAL *part_keys) {
+  __shared__ Shared sh;
+  const uint32_t n_full = a.n_vocab / T::kElems, n_chunk = (a.n_vocab + T::kElems - 1) / T::kElems;
+  const uint32_t c0 = blockIdx.x * part_chunks, c1 = min(n_chunk, c0 + part_chunks), c1_full = min(n_full, c1);
+  const uint32_t n_top = out.n_top;
+  for (uint32_t r = blockIdx.y; r < a.n_row; r += gridDim.y) {
+    const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
+    const uint8_t VL_GLOBAL *mask = kMask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
+    const int32_t token = a.token ? a.token[r] : 0;
+    if (token < 0) {
+      if (!parts) write_padding(out, r, threadIdx.x);
+      continue;
+    }
+    const float given = parts ? kNoLogit : given_logit<T>(a, r, token);
+    Sums sums = {kNoLogit, 0.0f, 0.0f};
+    uint32_t place = 0;
+    // kN chunks of this lane from c on, 256 apart
+    auto add = [&](auto n_of, const float (*x)[T::kElems], uint32_t c) {
+      constexpr uint32_t kN = decltype(n_of)::value;
+      float b[kN], m = kNoLogit;
+#pragma unroll
+      for (uint32_t u = 0; u < kN; ++u) {
+        b[u] = x[u][0];
+#pragma unroll
+        for (uint32_t j = 1; j < T::kElems; ++j) b[u] = fmaxf(b[u], x[u][j]);
+        m = fmaxf(m, b[u]);
+      }
+      if (n_top) {
+        uint32_t first = c + (kN - 1) * kThreads;
+#pragma unroll
+        for (uint32_t u = kN - 1; u-- > 0;) first = b[u] == m ? c + u * kThreads : first;
+        place = m > sums.m ? first : place;
+      }
+      sums = rebase(sums, fmaxf(sums.m, m), a.scale2);
+      const float ref = ref_of(sums.m);
+#pragma unroll
+      for (uint32_t u = 0; u < kN; ++u)
+#pragma unroll
+        for (uint32_t j = 0; j < T::kElems; ++j) {
+          const float z = (x[u][j] - ref) * a.scale2, e = __builtin_amdgcn_exp2f(z);
+          sums.s += e;
+          if (kEntropy) sums.y += e * fmaxf(z, kFar);
+        }
+    };
+    uint32_t c = c0;
+    for (; c + kBatch * kThreads <= c1_full; c += kBatch * kThreads) {
+      u32x4 w[kBatch];
+      uint32_t bits[kBatch];
+#pragma unroll
+      for (uint32_t u = 0; u < kBatch; ++u) w[u] = load_chunk<T>(row, c + threadIdx.x + u * kThreads);
+#pragma unroll
+      for (uint32_t u = 0; u < kBatch; ++u) bits[u] = kMask ? mask_bits<T>(mask, c + threadIdx.x + u * kThreads) : 0u;
+      float x[kBatch][T::kElems];
+#pragma unroll
+      for (uint32_t u = 0; u < kBatch; ++u) {
+        T::unpack(w[u], x[u]);
+        if (kMask) keep_allowed<T>(x[u], bits[u]);
+      }
+      add(std::integral_constant<uint32_t, kBatch>{}, x, c + threadIdx.x);
+    }
+    for (; c < c1; c += kThreads) {
+      float x[1][T::kElems];
+      if (c + threadIdx.x < c1) {
+        load_any<T>(a, row, mask, c + threadIdx.x, x[0]);
+        add(std::integral_constant<uint32_t, 1>{}, x, c + threadIdx.x);
+      }
+    }
+    const float mine = sums.m;
+    sums = join_sums(sh, sums, a.scale2);
+    Final f = {};
+    if (!parts) f = finish(a, out, r, sums, given, threadIdx.x == 0);
+    else if (threadIdx.x == 0) parts[(uint64_t)r * gridDim.x + blockIdx.x] = Part{sums.m, sums.s, sums.y, 0.0f};
+    if (n_top) {
+      const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      sh.key[threadIdx.x] = mine == kNoLogit ? 0ull : key_of(ordered(mine), place);
+      __syncthreads();
+      if (wave == 0) {
+        uint64_t k[kWaves];
+#pragma unroll
+        for (uint32_t i = 0; i < kWaves; ++i) k[i] = sh.key[lane + 64 * i];
+        const uint64_t least = nth_key<kWaves>(k, n_top);
+        uint32_t n_hot = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kWaves; ++i) {
+          const uint64_t is = __ballot(k[i] >= least);
+          if (k[i] >= least) sh.hot[n_hot + __popcll(is & ((1ull << lane) - 1ull))] = lane + 64 * i;
+          n_hot += __popcll(is);
+        }
+        if (lane == 0) {
+          sh.least = least;
+          sh.n_hot = n_hot;
+        }
+      }
+      __syncthreads();
+      List list;
+      const uint64_t least = sh.least;
+      for (uint32_t h = wave; h < sh.n_hot; h += kWaves) {
+        const uint32_t from = c0 + sh.hot[h];
+        for (uint32_t base = from; base < c1; base += 64 * kThreads) {
+          const uint32_t at = base + lane * kThreads;
+          float x[T::kElems];
+          if (at < c1) {
+            load_any<T>(a, row, mask, at, x);
+          } else {
+#pragma unroll
+            for (uint32_t j = 0; j < T::kElems; ++j) x[j] = kNoLogit;
+          }
+          list_chunk<T>(list, x, at, least, n_top);
+        }
+      }
+      const uint64_t best = join_lists(sh, list, n_top);
+      if (threadIdx.x < n_top) {
+        if (!parts) write_top(out, r, threadIdx.x, best, f);
+        else part_keys[((uint64_t)r * gridDim.x + blockIdx.x) * n_top + threadIdx.x] = best;
+      }
+    }
+    __syncthreads();   // (sh is used again)
+  }
+}
+
+// The parts of a row as one: a workgroup per row.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_scores_join(Rows a, Scores out, uint32_t n_part, const Part VL_GLOBAL *parts, const uint64_t VL_GLOBAL *part_keys) {
+  __shared__ Shared sh;
+  const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_top = out.n_top;
+  for (uint32_t r = blockIdx.x; r < a.n_row; r += gridDim.x) {
+    const int32_t token = a.token ? a.token[r] : 0;
+    if (token < 0) {
+      write_padding(out, r, threadIdx.x);
+      continue;
+    }
+    const float given = given_logit<T>(a, r, token);
+    Sums sums = {kNoLogit, 0.0f, 0.0f};
+    if (threadIdx.x < n_part) {   // (never more than there are threads)
+      const Part p = parts[(uint64_t)r * n_part + threadIdx.x];
+      sums = Sums{p.x, p.y, p.z};
+    }
+    sums = join_sums(sh, sums, a.scale2);
+    const Final f = finish(a, out, r, sums, given, threadIdx.x == 0);
+    if (n_top) {
+      List list;
+      const uint64_t VL_GLOBAL *keys = part_keys + (uint64_t)r * n_part * n_top;
+      for (uint32_t p = wave; p < n_part; p += kWaves) {
+        const uint64_t k = lane < n_top ? keys[(uint64_t)p * n_top + lane] : 0ull;
+        list.insert_lanes(k, k > list.worst, n_top);
+      }
+      const uint64_t best = join_lists(sh, list, n_top);
+      if (threadIdx.x < n_top) write_top(out, r, threadIdx.x, best, f);
+    }
     __syncthreads();
   }
-  v = room[0];
-  __syncthreads();
-  return v;
 }
 
+// ---- the gradient
+struct Grad {
+  const float VL_GLOBAL *stat, *entropy, *g_logprob, *g_entropy;
+  uint8_t VL_GLOBAL *grad;
+  uint64_t ld;   // in bytes
+};
+// What a row's elements need: with t = log2 p, d = p (t * slope + level), and `hot` more at the given token.
+struct GradRow { float ref, log2_sum, slope, level, hot; uint32_t token; bool idle; };
+__device__ inline GradRow grad_row(const Rows &a, const Grad &b, uint32_t r) {
+  GradRow g = {};
+  const int32_t token = a.token ? a.token[r] : 0;
+  const float m = b.stat[2ull * r], log_sum = b.stat[2ull * r + 1];
+  g.idle = token < 0 || m == kNoLogit;
+  if (g.idle) return g;
+  g.ref = m;
+  g.log2_sum = log_sum * kLog2e;
+  const float gl = b.g_logprob ? b.g_logprob[r] : 0.0f, e = b.g_entropy ? b.g_entropy[r] : 0.0f;
+  const float h = b.g_entropy ? b.entropy[r] : 0.0f;
+  g.slope = -a.scale * e * kLn2;
+  g.level = -a.scale * (gl + e * h);
+  g.hot = b.g_logprob ? gl * a.scale : 0.0f;
+  g.token = b.g_logprob ? (uint32_t)token : kNone;
+  return g;
+}
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_scores(Rows a, vl_token_scores out) {
-  __shared__ float sums[kThreads];
-  __shared__ Best bests[kThreads];
-  for (uint32_t r = blockIdx.x; r < a.n_row; r += gridDim.x) {
-    const int32_t token = a.token ? a.token[r] : 0;
-    const bool padding = token < 0;
-    const uint32_t n = padding ? 0u : a.n_vocab;
-    float m = kNoLogit;
-    for (uint32_t t = threadIdx.x; t < n; t += kThreads) m = fmaxf(m, logit<T>(a, r, t));
-    m = block_reduce(m, sums, [](float x, float y) { return fmaxf(x, y); });
-    const float from = m == kNoLogit ? 0.0f : m;
-    float s = 0, y = 0;
-    for (uint32_t t = threadIdx.x; t < n; t += kThreads) {
-      const float z = (logit<T>(a, r, t) - from) * a.scale, e = expf(z);
-      s += e;
-      y += e == 0.0f ? 0.0f : e * z;
+__device__ inline void grad_chunk(const Rows &a, const GradRow &g, uint32_t c, float *x, uint32_t bits, bool masked) {
+#pragma unroll
+  for (uint32_t j = 0; j < T::kElems; ++j) {
+    const float t = __builtin_fmaf(x[j] - g.ref, a.scale2, -g.log2_sum), p = __builtin_amdgcn_exp2f(t);
+    x[j] = p * __builtin_fmaf(fmaxf(t, kFar), g.slope, g.level);
+  }
+  if (g.token / T::kElems == c) {
+#pragma unroll
+    for (uint32_t j = 0; j < T::kElems; ++j) x[j] += g.token % T::kElems == j ? g.hot : 0.0f;
+  }
+  if (masked) {   // 0 where not allowed, whatever stood there
+#pragma unroll
+    for (uint32_t j = 0; j < T::kElems; ++j)
+      x[j] = as_float(as_word(x[j]) & (uint32_t)((int32_t)(bits << (31 - j)) >> 31));
+  }
+}
+template <class T>
+__device__ inline void store_any(const Rows &a, uint8_t VL_GLOBAL *to, uint32_t c, const float *x) {
+  const uint32_t from = c * T::kElems;
+  if (from + T::kElems <= a.n_vocab) {
+    *(typename T::chunk VL_GLOBAL *)(to + (uint64_t)c * 16) = T::pack(x);
+  } else {
+#pragma unroll
+    for (uint32_t j = 0; j < T::kElems; ++j)
+      if (from + j < a.n_vocab) ((typename T::type VL_GLOBAL *)to)[from + j] = T::narrow(x[j]);
+  }
+}
+
+template <class T, uint32_t kChunks>
+__global__ __launch_bounds__(kThreads) void k_grad_short(Rows a, Grad b) {
+  const uint32_t lane = threadIdx.x & 63u;
+  for (uint32_t r = blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < a.n_row; r += gridDim.x * kWaves) {
+    const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
+    uint8_t VL_GLOBAL *to = b.grad + (uint64_t)r * b.ld;
+    const uint8_t VL_GLOBAL *mask = a.mask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
+    const GradRow g = grad_row(a, b, r);
+    float x[kChunks][T::kElems];
+    uint32_t bits[kChunks];
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i) {
+      const uint32_t c = lane + 64 * i;
+      bits[i] = mask && !g.idle && c * T::kElems < a.n_vocab ? mask_bits<T>(mask, c) : 0u;
+      if (!g.idle) load_any<T>(a, row, nullptr, c, x[i]);
     }
-    auto add = [](float u, float v) { return u + v; };
-    s = block_reduce(s, sums, add);
-    y = block_reduce(y, sums, add);
-    const bool bad = s != s;
-    const float log_sum = logf(s);
-    if (threadIdx.x == 0) {
-      const bool in = !padding && (uint32_t)token < a.n_vocab;
-      const float x = a.token && in ? logit<T>(a, r, (uint32_t)token) : kNoLogit;
-      if (out.logprob) out.logprob[r] = padding ? 0.0f : bad ? s : x == kNoLogit ? kNoLogit : (x - from) * a.scale - log_sum;
-      if (out.entropy) out.entropy[r] = s == 0.0f ? 0.0f : log_sum - y / s;
-      if (out.stat) {
-        out.stat[2ull * r] = padding ? 0.0f : bad ? s : m;
-        out.stat[2ull * r + 1] = padding ? 0.0f : log_sum;
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i) {
+      if (g.idle) {
+#pragma unroll
+        for (uint32_t j = 0; j < T::kElems; ++j) x[i][j] = 0.0f;
+      } else {
+        grad_chunk<T>(a, g, lane + 64 * i, x[i], bits[i], mask != nullptr);
       }
-    }
-    Best last = {__builtin_huge_valf(), 0u};
-    for (uint32_t k = 0; k < out.n_top; ++k) {
-      Best b = {kNoLogit, kNone};
-      for (uint32_t t = threadIdx.x; t < n; t += kThreads) {
-        const Best c = {logit<T>(a, r, t), t};
-        if (c.x != kNoLogit && better(c, b) && better(last, c)) b = c;
-      }
-      last = b = block_reduce(b, bests, [](Best u, Best v) { return better(u, v) ? u : v; });
-      if (threadIdx.x == 0) {
-        const uint64_t at = (uint64_t)r * out.n_top + k;
-        const bool none = b.t == kNone;
-        if (out.top_token) out.top_token[at] = none || bad ? -1 : (int32_t)b.t;
-        if (out.top_logprob) out.top_logprob[at] = bad ? s : none ? kNoLogit : (b.x - from) * a.scale - log_sum;
-      }
+      store_any<T>(a, to, lane + 64 * i, x[i]);
     }
   }
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_score_grad(Rows a, const float *stat, const float *entropy, const float *g_logprob,
-                                                         const float *g_entropy, uint8_t *grad, uint64_t grad_ld) {
-  for (uint32_t r = blockIdx.x; r < a.n_row; r += gridDim.x) {
-    const int32_t token = a.token ? a.token[r] : 0;
-    typename T::type *to = (typename T::type *)(grad + (uint64_t)r * grad_ld);
-    const float m = stat[2ull * r], log_sum = stat[2ull * r + 1];
-    const bool none = token < 0 || m == kNoLogit;
-    const float g = none || !g_logprob ? 0.0f : g_logprob[r], e = none || !g_entropy ? 0.0f : g_entropy[r];
-    const float h = none || !g_entropy ? 0.0f : entropy[r];
-    for (uint32_t t = threadIdx.x; t < a.n_vocab; t += kThreads) {
-      float d = 0;
-      if (!none && (!a.mask || ((a.mask[(uint64_t)r * a.mask_ld + (t >> 5)] >> (t & 31u)) & 1u))) {
-        const float lp = (T::wide(((const typename T::type VL_GLOBAL *)(a.logits + (uint64_t)r * a.ld))[t]) - m) * a.scale - log_sum;
-        const float p = expf(lp);
-        d = g * ((t == (uint32_t)token ? 1.0f : 0.0f) - p) - (p == 0.0f ? 0.0f : e * p * (lp + h));
-        d *= a.scale;
+template <class T, bool kMask>
+__global__ __launch_bounds__(kThreads) void k_grad_long(Rows a, Grad b, uint32_t piece_chunks) {
+  const uint32_t n_full = a.n_vocab / T::kElems, n_chunk = (a.n_vocab + T::kElems - 1) / T::kElems;
+  const uint32_t c0 = blockIdx.x * piece_chunks, c1 = min(n_chunk, c0 + piece_chunks), c1_full = min(n_full, c1);
+  for (uint32_t r = blockIdx.y; r < a.n_row; r += gridDim.y) {
+    const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
+    uint8_t VL_GLOBAL *to = b.grad + (uint64_t)r * b.ld;
+    const uint8_t VL_GLOBAL *mask = kMask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
+    const GradRow g = grad_row(a, b, r);
+    uint32_t c = c0 + threadIdx.x;
+    if (g.idle) {
+      float x[T::kElems] = {};
+      for (; c < c1; c += kThreads) store_any<T>(a, to, c, x);
+      continue;
+    }
+    for (; c - threadIdx.x + kBatch * kThreads <= c1_full; c += kBatch * kThreads) {
+      u32x4 w[kBatch];
+      uint32_t bits[kBatch];
+#pragma unroll
+      for (uint32_t u = 0; u < kBatch; ++u) w[u] = load_chunk<T>(row, c + u * kThreads);
+#pragma unroll
+      for (uint32_t u = 0; u < kBatch; ++u) bits[u] = kMask ? mask_bits<T>(mask, c + u * kThreads) : 0u;
+#pragma unroll
+      for (uint32_t u = 0; u < kBatch; ++u) {
+        float x[T::kElems];
+        T::unpack(w[u], x);
+        grad_chunk<T>(a, g, c + u * kThreads, x, bits[u], kMask);
+        *(typename T::chunk VL_GLOBAL *)(to + (uint64_t)(c + u * kThreads) * 16) = T::pack(x);
       }
-      to[t] = T::narrow(d);
+    }
+    for (; c < c1; c += kThreads) {
+      float x[T::kElems];
+      load_any<T>(a, row, nullptr, c, x);
+      grad_chunk<T>(a, g, c, x, kMask ? mask_bits<T>(mask, c) : 0u, kMask);
+      store_any<T>(a, to, c, x);
     }
   }
 }
+
+// ---- host
 
 constexpr uint32_t kMostRows = 0x7FFFFFFFu;
+constexpr uint32_t kShortChunks = 256;   // 16-byte chunks of a row that one wavefront takes (four per lane)
+constexpr uint32_t kMostGridY = 65535;
 
 uint32_t size_of(uint32_t type) { return type == VL_F32 ? 4u : 2u; }
+uint32_t chunks_of(const vl_token_rows *a) { const uint32_t e = 16u / size_of(a->type); return (a->n_vocab + e - 1) / e; }
 
 int32_t check_rows(const vl_token_rows *a) {
   if (!a || !a->logits) return VL_E_NULL;
   if (a->type > VL_BF16) return VL_E_RANGE;
-  if (a->n_vocab == 0 || a->n_vocab > VL_MAX_VOCAB || !(a->scale > 0.0f) || a->scale > 3.402823466e38f) return VL_E_RANGE;
+  if (a->n_vocab == 0 || a->n_vocab > VL_MAX_VOCAB || !(a->scale >= VL_MIN_SCALE) || a->scale > 1.0f / VL_MIN_SCALE) return VL_E_RANGE;
   if (a->n_row == 0 || a->n_row > kMostRows || (a->n_row > 1 && a->ld < a->n_vocab)) return VL_E_SHAPE;
   if (a->mask && a->mask_ld && a->mask_ld < (a->n_vocab + 31) / 32) return VL_E_SHAPE;
   if (((uintptr_t)a->logits & (size_of(a->type) - 1)) || ((uintptr_t)a->mask & 3) || ((uintptr_t)a->token & 3)) return VL_E_SHAPE;
@@ -147,8 +677,55 @@ int32_t check_scores(const vl_token_rows *a, const vl_token_scores *o) {
 }
 
 Rows device_rows(const vl_token_rows *a) {
-  return Rows{(const uint8_t VL_GLOBAL *)a->logits, a->ld * size_of(a->type), (const uint32_t VL_GLOBAL *)a->mask, a->mask_ld,
-              (const int32_t VL_GLOBAL *)a->token, a->n_row, a->n_vocab, a->scale};
+  return Rows{(const uint8_t VL_GLOBAL *)a->logits, a->ld * size_of(a->type), (const uint8_t VL_GLOBAL *)a->mask, a->mask_ld * 4,
+              (const int32_t VL_GLOBAL *)a->token, a->n_row, a->n_vocab, a->scale, (float)((double)a->scale * 1.4426950408889634)};
+}
+
+// How many workgroups share a row, and how many chunks each takes
+struct Split { uint32_t parts, chunks; };
+constexpr uint32_t kWantGroups = 2048;    // eight per compute unit, as many as it holds
+constexpr uint32_t kLeastChunks = 512;    // of a part
+Split split_of(const vl_token_rows *a) {
+  const uint32_t n = chunks_of(a);
+  uint32_t parts = a->n_row >= kWantGroups ? 1u : kWantGroups / a->n_row;
+  const uint32_t most = n / kLeastChunks < kThreads ? n / kLeastChunks : kThreads;
+  if (parts > most) parts = most;
+  if (parts <= 1) return Split{1, n};
+  const uint32_t chunks = ((n + parts - 1) / parts + kThreads - 1) / kThreads * kThreads;
+  return Split{(n + chunks - 1) / chunks, chunks};
+}
+uint64_t work_of(const vl_token_rows *a, const vl_token_scores *o) {
+  if (chunks_of(a) <= kShortChunks) return 0;
+  const Split s = split_of(a);
+  return s.parts == 1 ? 0 : (uint64_t)a->n_row * s.parts * (sizeof(Part) + 8ull * o->n_top);
+}
+
+template <class T>
+void launch_scores(const Rows &a, const Scores &out, uint32_t n_chunk, Split split, void *work, hipStream_t stream) {
+  if (n_chunk <= kShortChunks) {
+    const uint32_t blocks = std::min((a.n_row + kWaves - 1) / kWaves, 1u << 20);
+    (n_chunk <= 64 ? k_scores_short<T, 1> : n_chunk <= 128 ? k_scores_short<T, 2> : k_scores_short<T, 4>)<<<blocks, kThreads, 0, stream>>>(a, out);
+    return;
+  }
+  Part VL_GLOBAL *parts = split.parts > 1 ? (Part VL_GLOBAL *)work : nullptr;
+  uint64_t VL_GLOBAL *keys = parts ? (uint64_t VL_GLOBAL *)((uint8_t *)work + (uint64_t)a.n_row * split.parts * sizeof(Part)) : nullptr;
+  const dim3 grid(split.parts, std::min(a.n_row, kMostGridY));
+  const bool entropy = out.entropy;
+  (a.mask ? entropy ? k_scores_long<T, true, true> : k_scores_long<T, true, false>
+          : entropy ? k_scores_long<T, false, true> : k_scores_long<T, false, false>)<<<grid, kThreads, 0, stream>>>(a, out, split.chunks, parts, keys);
+  if (parts) k_scores_join<T><<<a.n_row, kThreads, 0, stream>>>(a, out, split.parts, parts, keys);
+}
+
+template <class T>
+void launch_grad(const Rows &a, const Grad &b, uint32_t n_chunk, hipStream_t stream) {
+  if (n_chunk <= kShortChunks) {
+    const uint32_t blocks = std::min((a.n_row + kWaves - 1) / kWaves, 1u << 20);
+    (n_chunk <= 64 ? k_grad_short<T, 1> : n_chunk <= 128 ? k_grad_short<T, 2> : k_grad_short<T, 4>)<<<blocks, kThreads, 0, stream>>>(a, b);
+    return;
+  }
+  const uint32_t piece = kBatch * kThreads;
+  const dim3 grid((n_chunk + piece - 1) / piece, std::min(a.n_row, kMostGridY));
+  (a.mask ? k_grad_long<T, true> : k_grad_long<T, false>)<<<grid, kThreads, 0, stream>>>(a, b, piece);
 }
 
 }  // namespace
@@ -156,18 +733,22 @@ Rows device_rows(const vl_token_rows *a) {
 extern "C" int32_t vl_token_logprobs_work(const vl_token_rows *rows, const vl_token_scores *out, uint64_t *bytes) {
   if (!bytes) return VL_E_NULL;
   const int32_t rc = check_scores(rows, out);
-  if (rc == VL_OK) *bytes = 0;
+  if (rc == VL_OK) *bytes = work_of(rows, out);
   return rc;
 }
 
 extern "C" int32_t vl_token_logprobs(const vl_token_rows *rows, const vl_token_scores *out, void *work, uint64_t work_bytes, vl_stream stream_) {
   const int32_t rc = check_scores(rows, out);
   if (rc != VL_OK) return rc;
-  (void)work; (void)work_bytes;
+  if (const uint64_t need = work_of(rows, out)) {
+    if (!work) return VL_E_NULL;
+    if (work_bytes < need || (uintptr_t)work & 15) return VL_E_SHAPE;
+  }
   hipStream_t stream = (hipStream_t)stream_;
-  const Rows a = device_rows(rows);
-  const uint32_t blocks = a.n_row < 65536u ? a.n_row : 65536u;
-  (rows->type == VL_F32 ? k_scores<F32> : rows->type == VL_F16 ? k_scores<F16> : k_scores<BF16>)<<<blocks, kThreads, 0, stream>>>(a, *out);
+  const Scores o = {(float VL_GLOBAL *)out->logprob, (float VL_GLOBAL *)out->entropy, (float VL_GLOBAL *)out->stat, (float VL_GLOBAL *)out->top_logprob,
+                    (int32_t VL_GLOBAL *)out->top_token, out->n_top};
+  (rows->type == VL_F32 ? launch_scores<F32> : rows->type == VL_F16 ? launch_scores<F16> : launch_scores<BF16>)(
+      device_rows(rows), o, chunks_of(rows), split_of(rows), work, stream);
   VL_HIP(hipGetLastError());
   return VL_OK;
 }
@@ -181,10 +762,9 @@ extern "C" int32_t vl_token_logprobs_grad(const vl_token_rows *rows, const float
   if ((rows->n_row > 1 && grad_ld < rows->n_vocab) || (uintptr_t)grad & (size_of(rows->type) - 1)) return VL_E_SHAPE;
   if (((uintptr_t)stat | (uintptr_t)entropy | (uintptr_t)g_logprob | (uintptr_t)g_entropy) & 3) return VL_E_SHAPE;
   hipStream_t stream = (hipStream_t)stream_;
-  const Rows a = device_rows(rows);
-  const uint32_t blocks = a.n_row < 65536u ? a.n_row : 65536u;
-  (rows->type == VL_F32 ? k_score_grad<F32> : rows->type == VL_F16 ? k_score_grad<F16> : k_score_grad<BF16>)<<<blocks, kThreads, 0, stream>>>(
-      a, stat, entropy, g_logprob, g_entropy, (uint8_t *)grad, grad_ld * size_of(rows->type));
+  const Grad b = {(const float VL_GLOBAL *)stat, (const float VL_GLOBAL *)entropy, (const float VL_GLOBAL *)g_logprob, (const float VL_GLOBAL *)g_entropy,
+                  (uint8_t VL_GLOBAL *)grad, grad_ld * size_of(rows->type)};
+  (rows->type == VL_F32 ? launch_grad<F32> : rows->type == VL_F16 ? launch_grad<F16> : launch_grad<BF16>)(device_rows(rows), b, chunks_of(rows), stream);
   VL_HIP(hipGetLastError());
   return VL_OK;
 }
