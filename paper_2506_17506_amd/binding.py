@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -377,89 +378,97 @@ def vl_free_bases_multi(queries, masks, stream=None) -> None:
 
 VL_F32, VL_F16, VL_BF16 = 0, 1, 2
 VL_MAX_VOCAB, VL_MAX_TOP = 1 << 24, 32
-_TYPE = {"torch.float32": VL_F32, "torch.float16": VL_F16, "torch.bfloat16": VL_BF16}
-_WORDS = ("torch.int32", "torch.uint32")
 POLICY_STATS_DTYPE = np.dtype([("loss", "<f4"), ("kl", "<f4"), ("n_token", "<u8"), ("n_clipped", "<u8")])   # vl_policy_stats
+# the structures' fields as bytes, which is quicker than a ctypes structure per call
+_PACK_ROWS = struct.Struct("<QQQQQIIIf").pack
+_PACK_SCORES = struct.Struct("<QQQQQII").pack
+_PACK_WEIGHTS = struct.Struct("<ffff").pack
+_PACK_BATCH = struct.Struct("<QQQQQQQQIIfffI").pack
 
 
-def _need(what, ok, code=-2):
-    if not ok:
-        raise VlError(code, what)
+class _Torch:
+    """what of torch the calls below need, looked up once"""
+    def __init__(self):
+        import torch
+        self.empty, self.uint8 = torch.empty, torch.uint8
+        self.type = {torch.float32: VL_F32, torch.float16: VL_F16, torch.bfloat16: VL_BF16}
+        self.f32 = (torch.float32,)
+        self.words = (torch.int32, torch.uint32)
+        self.longs = (torch.int64, torch.uint64)
+        self.record = (torch.uint8, torch.int32, torch.uint32, torch.int64)
+        self.device = torch.cuda.current_device
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.stream = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        self.on, self.external = torch.cuda.stream, torch.cuda.ExternalStream
 
 
-def _tensor(what, x, dtypes, shape=None, nullable=True):
-    """The pointer of a contiguous tensor of one of the types (and of that shape), None for None."""
+_t = None
+
+
+def _device_of(x, what):
+    """the current device, which `x` has to be on (tensors of the host and of other devices are refused)"""
+    global _t
     if x is None:
-        _need(what, nullable, -1)
-        return None
-    _here(what, x)
-    _need(what, str(x.dtype) in dtypes, -3)
-    _need(what, x.is_contiguous() and (shape is None or tuple(x.shape) == shape))
+        raise VlError(-1, what)
+    if _t is None:
+        load()
+        _t = _Torch()
+    if x.is_cuda and x.get_device() == _t.device():
+        return x.get_device()
+    raise VlError(-7, what)
+
+
+def _tensor(what, x, dtypes, shape, device, nullable=True):
+    """The pointer of a contiguous tensor of one of the types and that shape (None: of any) on that device, 0 for None."""
+    if x is None:
+        if nullable:
+            return 0
+        raise VlError(-1, what)
+    if x.get_device() != device:
+        raise VlError(-7, what)
+    if x.dtype not in dtypes:
+        raise VlError(-3, what)
+    if (shape is not None and x.shape != shape) or not x.is_contiguous():
+        raise VlError(-2, what)
     return x.data_ptr()
 
 
-_current_device = None
-
-
-def _here(what, x):
-    """tensors of another device than the current one, and of the host, are refused"""
-    global _current_device
-    if _current_device is None:
-        import torch
-        _current_device = torch.cuda.current_device
-    d = x.device
-    _need(what, d.type == "cuda" and d.index == _current_device(), -7)
+def _row_pitch(what, x):
+    """distance of the rows of a matrix whose rows are contiguous"""
+    if x.dim() == 2:
+        ld, step = x.stride()
+        if step == 1 or x.shape[1] <= 1:
+            return ld
+    raise VlError(-2, what)
 
 
 def _token_rows(what, logits, token, mask, scale):
-    _here(what, logits)
-    _need(what, str(logits.dtype) in _TYPE, -3)
-    _need(what, logits.dim() == 2 and (logits.shape[1] <= 1 or logits.stride(1) == 1))
+    """(vl_token_rows as bytes, n_row, n_vocab, device)"""
+    device = _device_of(logits, what)
+    kind = _t.type.get(logits.dtype)
+    if kind is None:
+        raise VlError(-3, what)
+    ld = _row_pitch(what, logits)
     n, v = logits.shape
-    a = _TokenRows(logits.data_ptr(), logits.stride(0), None, 0, None, n, v, _TYPE[str(logits.dtype)], scale)
+    p_mask = mask_ld = 0
     if mask is not None:
-        _here(what, mask)
-        _need(what, str(mask.dtype) in _WORDS, -3)
+        if mask.get_device() != device:
+            raise VlError(-7, what)
+        if mask.dtype not in _t.words:
+            raise VlError(-3, what)
         shared = mask.dim() == 1
-        _need(what, mask.dim() in (1, 2) and mask.stride(-1) == 1 and mask.shape[-1] * 32 >= v and (shared or mask.shape[0] == n))
-        a.mask, a.mask_ld = mask.data_ptr(), 0 if shared or n == 1 else mask.stride(0)
-    a.token = _tensor(what, token, ("torch.int32",), (n,))
-    return a
+        if not (shared or (mask.dim() == 2 and mask.shape[0] == n)) or mask.shape[-1] * 32 < v or (mask.stride(-1) != 1 and mask.shape[-1] > 1):
+            raise VlError(-2, what)
+        p_mask, mask_ld = mask.data_ptr(), 0 if shared or n == 1 else mask.stride(0)
+    p_token = 0 if token is None else _tensor(what, token, _t.words[:1], (n,), device)
+    return _PACK_ROWS(logits.data_ptr(), ld, p_mask, mask_ld, p_token, n, v, kind, scale), n, v, device
 
 
-def _work(n_bytes, stream, device):
-    """memory for one call on the stream it runs on"""
-    import torch
-    if stream is None:
-        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
-    if not hasattr(stream, "cuda_stream"):
-        stream = torch.cuda.ExternalStream(int(getattr(stream, "value", stream) or 0), device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+def _call_stream(stream, device):
+    return _t.stream(device) if stream is None else int(getattr(stream, "cuda_stream", getattr(stream, "value", stream)) or 0)
 
 
-def _work_bytes(what, call, work, stream, device, *args):
-    """(pointer, bytes, the tensor) of what `call` says the call needs: `work` or memory of the call's own"""
-    need = C.c_uint64()
-    rc = call(*args, C.byref(need))
-    if rc != 0:
-        raise VlError(rc, what)
-    if work is not None:
-        _here(what, work)
-        _need(what, work.is_contiguous())
-    elif need.value:
-        work = _work(need.value, stream, device)
-    return (None, 0, None) if work is None else (work.data_ptr(), work.numel() * work.element_size(), work)
-
-
-def vl_token_logprobs_work(logits, token=None, mask=None, scale=1.0, logprob=None, entropy=None, stat=None, top_token=None,
-                           top_logprob=None) -> int:
-    """Bytes of work that vl_token_logprobs needs for the same arguments."""
-    a, o = _token_scores(logits, token, mask, scale, logprob, entropy, stat, top_token, top_logprob)
-    return _work_bytes_only("vl_token_logprobs_work", load().vl_token_logprobs_work, C.byref(a), C.byref(o))
-
-
-def _work_bytes_only(what, call, *args):
+def _bytes_of(what, call, *args):
     need = C.c_uint64()
     rc = call(*args, C.byref(need))
     if rc != 0:
@@ -467,16 +476,42 @@ def _work_bytes_only(what, call, *args):
     return need.value
 
 
+def _work(what, n_bytes, work, stream, device):
+    """(pointer, bytes, the tensor): `work`, or n_bytes of the call's own, allocated on the stream it runs on"""
+    if work is not None:
+        if work.get_device() != device:
+            raise VlError(-7, what)
+        if not work.is_contiguous():
+            raise VlError(-2, what)
+    elif not n_bytes:
+        return None, 0, None
+    elif stream is None:
+        work = _t.empty(n_bytes, dtype=_t.uint8, device=device)
+    else:
+        with _t.on(stream if hasattr(stream, "cuda_stream") else _t.external(_call_stream(stream, device), device=device)):
+            work = _t.empty(n_bytes, dtype=_t.uint8, device=device)
+    return work.data_ptr(), work.numel() * work.element_size(), work
+
+
 def _token_scores(logits, token, mask, scale, logprob, entropy, stat, top_token, top_logprob):
+    """(vl_token_rows, vl_token_scores as bytes, device)"""
     what = "vl_token_logprobs"
-    a = _token_rows(what, logits, token, mask, scale)
-    n, f = a.n_row, ("torch.float32",)
+    rows, n, _, device = _token_rows(what, logits, token, mask, scale)
+    f, k = _t.f32, 0
     some = top_token if top_token is not None else top_logprob
-    _need(what, some is None or some.dim() == 2)
-    k = 0 if some is None else some.shape[1]
-    o = _TokenScores(_tensor(what, logprob, f, (n,)), _tensor(what, entropy, f, (n,)), _tensor(what, stat, f, (n, 2)),
-                     _tensor(what, top_token, ("torch.int32",), (n, k)), _tensor(what, top_logprob, f, (n, k)), k, 0)
-    return a, o
+    if some is not None:
+        if some.dim() != 2:
+            raise VlError(-2, what)
+        k = some.shape[1]
+    return rows, _PACK_SCORES(_tensor(what, logprob, f, (n,), device), _tensor(what, entropy, f, (n,), device), _tensor(what, stat, f, (n, 2), device),
+                              _tensor(what, top_token, _t.words[:1], (n, k), device), _tensor(what, top_logprob, f, (n, k), device), k, 0), device
+
+
+def vl_token_logprobs_work(logits, token=None, mask=None, scale=1.0, logprob=None, entropy=None, stat=None, top_token=None,
+                           top_logprob=None) -> int:
+    """Bytes of work that vl_token_logprobs needs for the same arguments."""
+    rows, out, _ = _token_scores(logits, token, mask, scale, logprob, entropy, stat, top_token, top_logprob)
+    return _bytes_of("vl_token_logprobs_work", load().vl_token_logprobs_work, rows, out)
 
 
 def vl_token_logprobs(logits, token=None, mask=None, scale=1.0, logprob=None, entropy=None, stat=None, top_token=None,
@@ -485,12 +520,12 @@ def vl_token_logprobs(logits, token=None, mask=None, scale=1.0, logprob=None, en
     one); token int32 [n_row]; mask int32 words [n_row, words] or [words] for all rows.  Written, those that are given:
     logprob, entropy float32 [n_row], stat float32 [n_row, 2], top_token int32 and top_logprob float32 [n_row, n_top].
     work: memory of vl_token_logprobs_work bytes, allocated on the call's stream if not given."""
-    a, o = _token_scores(logits, token, mask, scale, logprob, entropy, stat, top_token, top_logprob)
-    L = load()
-    p, n_bytes, keep = _work_bytes("vl_token_logprobs", L.vl_token_logprobs_work, work, stream, logits.device, C.byref(a), C.byref(o))
-    rc = L.vl_token_logprobs(C.byref(a), C.byref(o), p, n_bytes, _stream_ptr(stream))
+    what = "vl_token_logprobs"
+    rows, out, device = _token_scores(logits, token, mask, scale, logprob, entropy, stat, top_token, top_logprob)
+    p, n_bytes, keep = _work(what, 0 if work is not None else _bytes_of(what, _lib.vl_token_logprobs_work, rows, out), work, stream, device)
+    rc = _lib.vl_token_logprobs(rows, out, p, n_bytes, _call_stream(stream, device))
     if rc != 0:
-        raise VlError(rc, "vl_token_logprobs")
+        raise VlError(rc, what)
 
 
 def vl_token_logprobs_grad(logits, stat, grad, token=None, mask=None, scale=1.0, entropy=None, g_logprob=None, g_entropy=None,
@@ -498,14 +533,19 @@ def vl_token_logprobs_grad(logits, stat, grad, token=None, mask=None, scale=1.0,
     """grad [n_row, n_vocab] of the logits' type and any pitch, or logits itself; stat and entropy as vl_token_logprobs wrote
     them for the same rows; g_logprob, g_entropy float32 [n_row]."""
     what = "vl_token_logprobs_grad"
-    a = _token_rows(what, logits, token, mask, scale)
-    _here(what, grad)
-    _need(what, grad.dtype == logits.dtype, -3)
-    _need(what, grad.shape == logits.shape and (grad.shape[1] <= 1 or grad.stride(1) == 1))
-    f, n = ("torch.float32",), (a.n_row,)
-    rc = load().vl_token_logprobs_grad(C.byref(a), _tensor(what, stat, f, (a.n_row, 2)), _tensor(what, entropy, f, n),
-                                       _tensor(what, g_logprob, f, n), _tensor(what, g_entropy, f, n), grad.data_ptr(),
-                                       grad.stride(0), _stream_ptr(stream))
+    rows, n, _, device = _token_rows(what, logits, token, mask, scale)
+    if grad is None:
+        raise VlError(-1, what)
+    if grad.get_device() != device:
+        raise VlError(-7, what)
+    if grad.dtype != logits.dtype:
+        raise VlError(-3, what)
+    if grad.shape != logits.shape:
+        raise VlError(-2, what)
+    f = _t.f32
+    rc = _lib.vl_token_logprobs_grad(rows, _tensor(what, stat, f, (n, 2), device), _tensor(what, entropy, f, (n,), device),
+                                     _tensor(what, g_logprob, f, (n,), device), _tensor(what, g_entropy, f, (n,), device),
+                                     grad.data_ptr(), _row_pitch(what, grad), _call_stream(stream, device))
     if rc != 0:
         raise VlError(rc, what)
 
@@ -514,37 +554,42 @@ def vl_group_advantages(counts, group_off, weights, eps, advantage, reward=None,
     """counts: the records vl_count_violations_multi wrote (int32 [n, 8] or 32 n bytes) or None; group_off int32 [n_group + 1];
     weights: (ok, cons, real, safe); advantage, reward, extra float32 [n]."""
     what = "vl_group_advantages"
-    f = ("torch.float32",)
-    some = next((x for x in (advantage, reward, extra) if x is not None), None)
-    _need(what, some is not None, -1)
-    n = some.numel()
-    p = _tensor(what, counts, ("torch.int32", "torch.uint32", "torch.uint8"))
-    _need(what, counts is None or counts.numel() * counts.element_size() == 32 * n)
-    off = _tensor(what, group_off, _WORDS, nullable=False)
-    w = _RewardWeights(*weights)
-    rc = load().vl_group_advantages(p, _tensor(what, extra, f, (n,)), n, off, max(0, group_off.numel() - 1), C.byref(w), eps,
-                                    _tensor(what, reward, f, (n,)), _tensor(what, advantage, f, (n,)), _stream_ptr(stream))
+    device = _device_of(group_off, what)
+    some = advantage if advantage is not None else reward if reward is not None else extra
+    if some is None:
+        raise VlError(-1, what)
+    shape, n, f = some.shape, some.numel(), _t.f32
+    p = _tensor(what, counts, _t.record, None, device)
+    if counts is not None and counts.numel() * counts.element_size() != 32 * n:
+        raise VlError(-2, what)
+    rc = _lib.vl_group_advantages(p, _tensor(what, extra, f, shape, device), n, _tensor(what, group_off, _t.words, None, device),
+                                  max(0, group_off.numel() - 1), _PACK_WEIGHTS(*weights), eps, _tensor(what, reward, f, shape, device),
+                                  _tensor(what, advantage, f, shape, device), _call_stream(stream, device))
     if rc != 0:
         raise VlError(rc, what)
 
 
 def _policy_batch(logprob, logprob_old, start, length, advantage, weight, log_lo, log_hi, logprob_ref, kl, max_len):
+    """(vl_policy_batch as bytes, device)"""
     what = "vl_policy_loss"
-    f = ("torch.float32",)
-    _need(what, start is not None and logprob is not None, -1)
-    n, m = tuple(logprob.shape), (start.numel(),)
-    if max_len is None:   # the samples' mean, at most: a launch's shape, not a bound
-        max_len = min(0xFFFFFFFF, logprob.numel() // max(1, m[0]) + 1)
-    return _PolicyBatch(_tensor(what, logprob, f), _tensor(what, logprob_old, f, n, False), _tensor(what, logprob_ref, f, n),
-                        logprob.numel(), _tensor(what, start, ("torch.int64", "torch.uint64"), m), _tensor(what, length, _WORDS, m, False),
-                        _tensor(what, advantage, f, m, False), _tensor(what, weight, f, m, False), m[0], max_len, log_lo, log_hi, kl, 0)
+    device = _device_of(logprob, what)
+    if start is None:
+        raise VlError(-1, what)
+    f, shape, samples, n = _t.f32, logprob.shape, start.shape, logprob.numel()
+    m = start.numel()
+    if max_len is None:   # the mean length, if there is no room between the samples: a launch's shape, not a bound
+        max_len = min(0xFFFFFFFF, n // max(1, m) + 1)
+    return _PACK_BATCH(_tensor(what, logprob, f, None, device), _tensor(what, logprob_old, f, shape, device, False),
+                       _tensor(what, logprob_ref, f, shape, device), n, _tensor(what, start, _t.longs, None, device),
+                       _tensor(what, length, _t.words, samples, device, False), _tensor(what, advantage, f, samples, device, False),
+                       _tensor(what, weight, f, samples, device, False), m, max_len, log_lo, log_hi, kl, 0), device
 
 
 def vl_policy_loss_work(logprob, logprob_old, start, length, advantage, weight, log_lo, log_hi, logprob_ref=None, kl=0.0,
                         max_len=None) -> int:
     """Bytes of work that vl_policy_loss needs for the same arguments."""
-    b = _policy_batch(logprob, logprob_old, start, length, advantage, weight, log_lo, log_hi, logprob_ref, kl, max_len)
-    return _work_bytes_only("vl_policy_loss_work", load().vl_policy_loss_work, C.byref(b))
+    batch, _ = _policy_batch(logprob, logprob_old, start, length, advantage, weight, log_lo, log_hi, logprob_ref, kl, max_len)
+    return _bytes_of("vl_policy_loss_work", load().vl_policy_loss_work, batch)
 
 
 def vl_policy_loss(logprob, logprob_old, start, length, advantage, weight, grad, stats, log_lo, log_hi, logprob_ref=None, kl=0.0,
@@ -552,13 +597,13 @@ def vl_policy_loss(logprob, logprob_old, start, length, advantage, weight, grad,
     """logprob, logprob_old, logprob_ref, grad: float32 of one shape; start int64, length int32, advantage, weight float32
     [n_sample]; stats: device buffer of one POLICY_STATS_DTYPE record (24 bytes); max_len: the longest sample if known."""
     what = "vl_policy_loss"
-    b = _policy_batch(logprob, logprob_old, start, length, advantage, weight, log_lo, log_hi, logprob_ref, kl, max_len)
-    p_grad = _tensor(what, grad, ("torch.float32",), tuple(logprob.shape), False)
-    p_stats = _tensor(what, stats, ("torch.uint8", "torch.int32", "torch.int64"), nullable=False)
-    _need(what, stats.numel() * stats.element_size() >= 24)
-    L = load()
-    p, n_bytes, keep = _work_bytes(what, L.vl_policy_loss_work, work, stream, logprob.device, C.byref(b))
-    rc = L.vl_policy_loss(C.byref(b), p_grad, p_stats, p, n_bytes, _stream_ptr(stream))
+    batch, device = _policy_batch(logprob, logprob_old, start, length, advantage, weight, log_lo, log_hi, logprob_ref, kl, max_len)
+    p_grad = _tensor(what, grad, _t.f32, logprob.shape, device, False)
+    p_stats = _tensor(what, stats, _t.record, None, device, False)
+    if stats.numel() * stats.element_size() < 24:
+        raise VlError(-2, what)
+    p, n_bytes, keep = _work(what, 0 if work is not None else _bytes_of(what, _lib.vl_policy_loss_work, batch), work, stream, device)
+    rc = _lib.vl_policy_loss(batch, p_grad, p_stats, p, n_bytes, _call_stream(stream, device))
     if rc != 0:
         raise VlError(rc, what)
 

@@ -10,8 +10,8 @@
 //
 // The n best of a row cost the loop next to nothing: a lane also keeps which of its chunks its m came from.  The n lanes
 // with the best (m, chunk) hold all of the row's n best: any other lane's best is below n
-// larger ones.  Their chunks, n / 256 of the row, are read again, and what is not below the worst of those n maxima is put
-// into a sorted list that a wavefront's lanes hold, an entry each.
+// larger ones.  Their chunks, n / 256 of the row, are read again, and what is not below the worst of those n maxima, seldom more
+// than n logits, is put in order by counting, for each, how many are better.
 #include <algorithm>
 #include <type_traits>
 
@@ -47,7 +47,7 @@ __device__ inline uint32_t as_word(float x) { return __builtin_bit_cast(uint32_t
 struct F32 {
   typedef float type;
   typedef u32x4 chunk __attribute__((aligned(4)));
-  static constexpr uint32_t kElems = 4;
+  static constexpr uint32_t kElems = 4, kBits = 32;
   static __device__ inline float wide(float x) { return x; }
   static __device__ inline float narrow(float x) { return x; }
   static __device__ inline void unpack(u32x4 w, float *x) {
@@ -65,7 +65,7 @@ struct F16 {
   typedef _Float16 type;
   typedef _Float16 pair __attribute__((ext_vector_type(2)));
   typedef u32x4 chunk __attribute__((aligned(2)));
-  static constexpr uint32_t kElems = 8;
+  static constexpr uint32_t kElems = 8, kBits = 19;   // sign, the exponent of 32 bits, ten bits
   static __device__ inline float wide(_Float16 x) { return (float)x; }
   static __device__ inline _Float16 narrow(float x) { return (_Float16)x; }
   static __device__ inline void unpack(u32x4 w, float *x) {
@@ -88,7 +88,7 @@ struct BF16 {
   typedef __bf16 type;
   typedef __bf16 pair __attribute__((ext_vector_type(2)));
   typedef u32x4 chunk __attribute__((aligned(2)));
-  static constexpr uint32_t kElems = 8;
+  static constexpr uint32_t kElems = 8, kBits = 16;
   static __device__ inline float wide(__bf16 x) { return (float)x; }
   static __device__ inline __bf16 narrow(float x) { return (__bf16)x; }
   static __device__ inline void unpack(u32x4 w, float *x) {
@@ -169,15 +169,65 @@ __device__ inline Sums rebase(Sums from, float m, float scale2) {
   return Sums{m, from.s * f, f * (from.y + d * from.s)};
 }
 
-// ---- the best: logits with their tokens as one number, larger = better (a larger logit, or an equal one of a lower token)
+// ---- the best: a logit and its place as one number, larger = better (a larger logit, or an equal one of a lower place).  A
+// logit's order takes kBits of the upper word, as many as its type tells apart.
+template <class T>
 __device__ inline uint32_t ordered(float x) {
   const uint32_t b = as_word(x + 0.0f);   // (one zero)
-  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+  return (b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) >> (32 - T::kBits);
 }
-__device__ inline float unordered(uint32_t u) { return as_float(u ^ ((u >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
+template <class T>
+__device__ inline float unordered(uint32_t u) {
+  u <<= 32 - T::kBits;
+  return as_float(u >> 31 ? u ^ 0x80000000u : ~(u | ((1ull << (32 - T::kBits)) - 1)));
+}
 __device__ inline uint64_t key_of(uint32_t value, uint32_t place) { return ((uint64_t)value << 32) | (uint32_t)~place; }
 __device__ inline uint64_t lane_key(uint64_t k, uint32_t lane) {
   return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
+}
+
+// A number that at least n of the keys which a wavefront's lanes hold (kEach per lane, 0: none, the others all differ) reach, and at
+// most `most` >= n of them; 1 if there are fewer than n.  Bit by bit from the top; places are below 2^place_bits.
+template <uint32_t kBits, uint32_t kEach>
+__device__ inline uint64_t nth_key(const uint64_t *k, uint32_t place_bits, uint32_t n, uint32_t most) {
+  uint64_t least = 0;
+  auto count_from = [&](uint64_t attempt) {
+    uint32_t count = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) count += __popcll(__ballot(k[i] >= attempt));
+    return count;
+  };
+  for (int32_t bit = 31 + kBits; bit >= 32; --bit) {
+    const uint64_t attempt = least | (1ull << bit);
+    const uint32_t count = count_from(attempt);
+    if (count < n) continue;
+    least = attempt;
+    if (count <= most) return least;
+  }
+  if (!least) return 1ull;
+  least |= 0xFFFFFFFFull & ~((1ull << place_bits) - 1ull);   // (the same in every key)
+  for (int32_t bit = (int32_t)place_bits - 1; bit >= 0; --bit) {
+    const uint64_t attempt = least | (1ull << bit);
+    const uint32_t count = count_from(attempt);
+    if (count < n) continue;
+    least = attempt;
+    if (count <= most) return least;
+  }
+  return least;
+}
+__device__ inline uint32_t bits_for(uint32_t n) { return 32u - (uint32_t)__builtin_clz(n | 1u); }   // of numbers up to n
+
+// Where keys that may be among a row's n best are gathered.  More than there is room for are possible (many equal
+// logits, or a row sorted in an unlucky way); then the row's best are found by insertion instead.
+constexpr uint32_t kRoom = 256;
+constexpr uint32_t kMoreHot = 8;   // lanes whose chunks are read again beyond n, so that the search for them ends sooner
+struct Room {
+  uint64_t key[kRoom];
+  uint32_t n;
+};
+__device__ inline void gather(Room &room, uint64_t key) {
+  const uint32_t at = atomicAdd(&room.n, 1u);   // (their order does not matter)
+  if (at < kRoom) room.key[at] = key;
 }
 
 // A sorted list, entry i in lane i, 0 where there is none; `worst` is entry n - 1.
@@ -199,31 +249,14 @@ struct List {
   }
 };
 
-// The n-th largest of the keys that a wavefront's lanes hold, kEach per lane, bit by bit from the top, until no more
-// than n are at or above it; 1 if there are fewer than n (0: no key).  All keys but 0 differ.
-template <uint32_t kEach>
-__device__ inline uint64_t nth_key(const uint64_t *k, uint32_t n) {
-  uint64_t least = 0;
-  for (int32_t bit = 63; bit >= 0; --bit) {
-    const uint64_t attempt = least | (1ull << bit);
-    uint32_t count = 0;
-#pragma unroll
-    for (uint32_t i = 0; i < kEach; ++i) count += __popcll(__ballot(k[i] >= attempt));
-    if (count < n) continue;
-    least = attempt;
-    if (count == n) break;
-  }
-  return least ? least : 1ull;
-}
-
-// A chunk's logits that can be among the n best go into the list: `least` is a lane's (value, chunk) that n lanes' best reach
-template <class T>
-__device__ inline void list_chunk(List &list, const float *x, uint32_t c, uint64_t least, uint32_t n) {
+// f(key) for those of a chunk's logits that are at or above `least`, a (value, chunk), and so may be among the best
+template <class T, class F>
+__device__ inline void each_candidate(const float *x, uint32_t c, uint64_t least, F f) {
   const uint32_t value = (uint32_t)(least >> 32) + (c <= (uint32_t)~least ? 0u : 1u);
 #pragma unroll
   for (uint32_t j = 0; j < T::kElems; ++j) {
-    const uint32_t u = ordered(x[j]);
-    list.insert_lanes(key_of(u, c * T::kElems + j), x[j] != kNoLogit && u >= value, n);
+    const uint32_t u = ordered<T>(x[j]);
+    f(key_of(u, c * T::kElems + j), x[j] != kNoLogit && u >= value);
   }
 }
 
@@ -244,10 +277,11 @@ __device__ inline Final finish(const Rows &a, const Scores &out, uint32_t r, Sum
   }
   return f;
 }
+template <class T>
 __device__ inline void write_top(const Scores &out, uint32_t r, uint32_t k, uint64_t key, const Final &f) {
   const uint64_t at = (uint64_t)r * out.n_top + k;
   if (out.top_token) out.top_token[at] = key && !f.bad ? (int32_t)~(uint32_t)key : -1;
-  if (out.top_logprob) out.top_logprob[at] = f.bad ? f.s : key ? logprob_of(f, unordered((uint32_t)(key >> 32))) : kNoLogit;
+  if (out.top_logprob) out.top_logprob[at] = f.bad ? f.s : key ? logprob_of(f, unordered<T>((uint32_t)(key >> 32))) : kNoLogit;
 }
 // a row of padding; `lane` of 64 or more
 __device__ inline void write_padding(const Scores &out, uint32_t r, uint32_t lane) {
@@ -256,7 +290,7 @@ __device__ inline void write_padding(const Scores &out, uint32_t r, uint32_t lan
     if (out.entropy) out.entropy[r] = 0.0f;
     if (out.stat) out.stat[2ull * r] = out.stat[2ull * r + 1] = 0.0f;
   }
-  if (lane < out.n_top) write_top(out, r, lane, 0, Final{0, 0, 0, 0, false});
+  if (lane < out.n_top) write_top<F32>(out, r, lane, 0, Final{0, 0, 0, 0, false});
 }
 // the given token's logit, -infinity if there is none
 template <class T>
@@ -269,8 +303,9 @@ __device__ inline float given_logit(const Rows &a, uint32_t r, int32_t token) {
 // Short rows: a wavefront per row, kChunks chunks per lane, all in registers.
 template <class T, uint32_t kChunks>
 __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
-  const uint32_t lane = threadIdx.x & 63u;
-  for (uint32_t r = blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < a.n_row; r += gridDim.x * kWaves) {
+  __shared__ uint64_t room[kWaves][64];
+  const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (uint32_t r = blockIdx.x * kWaves + wave; r < a.n_row; r += gridDim.x * kWaves) {
     const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
     const uint8_t VL_GLOBAL *mask = a.mask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
     const int32_t token = a.token ? a.token[r] : 0;
@@ -306,12 +341,34 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
     if (out.entropy) sums.y = wave_sum(sums.y);
     const Final f = finish(a, out, r, sums, given, lane == 0);
     if (out.n_top) {
-      const uint64_t key = m == kNoLogit ? 0ull : key_of(ordered(m), place);
-      const uint64_t least = nth_key<1>(&key, out.n_top);
-      List list;
+      const uint32_t n = out.n_top;
+      const uint64_t key = m == kNoLogit ? 0ull : key_of(ordered<T>(m), place);
+      const uint64_t least = nth_key<T::kBits, 1>(&key, bits_for(64 * kChunks - 1), n, n + kMoreHot);
+      // gathered in the order of the lanes; up to 64 of them, usual unless many are equal, one per lane
+      uint32_t found = 0;
 #pragma unroll
-      for (uint32_t i = 0; i < kChunks; ++i) list_chunk<T>(list, x[i], lane + 64 * i, least, out.n_top);
-      if (lane < out.n_top) write_top(out, r, lane, list.key, f);
+      for (uint32_t i = 0; i < kChunks; ++i)
+        each_candidate<T>(x[i], lane + 64 * i, least, [&](uint64_t k, bool is) {
+          const uint64_t all = __ballot(is);
+          if (!all) return;
+          const uint32_t at = found + __popcll(all & ((1ull << lane) - 1ull));
+          if (is && at < 64) room[wave][at] = k;
+          found += __popcll(all);
+        });
+      if (found <= 64) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");   // (written and read by one wavefront)
+        const uint64_t mine = lane < found ? room[wave][lane] : 0ull;
+        uint32_t rank = 0;
+        for (uint32_t i = 0; i < found; ++i) rank += lane_key(mine, i) > mine;
+        if (lane < found && rank < n) write_top<T>(out, r, rank, mine, f);
+        if (lane >= found && lane < n) write_top<T>(out, r, lane, 0, f);
+      } else {
+        List list;
+#pragma unroll
+        for (uint32_t i = 0; i < kChunks; ++i)
+          each_candidate<T>(x[i], lane + 64 * i, least, [&](uint64_t k, bool is) { list.insert_lanes(k, is, n); });
+        if (lane < n) write_top<T>(out, r, lane, list.key, f);
+      }
     }
   }
 }
@@ -321,32 +378,57 @@ typedef float Part __attribute__((ext_vector_type(4)));
 
 struct Shared {
   Sums sums[kWaves];
+  Room room;
   uint64_t key[kThreads];
-  uint64_t list[kWaves][VL_MAX_TOP];
+  uint64_t list[kWaves * VL_MAX_TOP];
   uint64_t least;
-  uint32_t n_hot, hot[VL_MAX_TOP];
+  uint32_t n_hot, hot[VL_MAX_TOP + kMoreHot];
 };
 
-// the wavefronts' lists as one, best first: entry k of it in thread k < n_top; by rank, since all keys differ
+// The n best of `found` <= kRoom different keys, best first: entry k in thread k < n, 0 where there are fewer
+__device__ inline uint64_t in_order(const uint64_t *keys, uint32_t found, uint64_t *out, uint32_t n) {
+  const uint64_t mine = threadIdx.x < found ? keys[threadIdx.x] : 0ull;
+  uint32_t rank = 0;
+  if (threadIdx.x < found)
+    for (uint32_t i = 0; i < found; ++i) rank += keys[i] > mine;
+  if (threadIdx.x < found && mine && rank < n) out[rank] = mine;
+  __syncthreads();
+  return threadIdx.x < n && threadIdx.x < found ? out[threadIdx.x] : 0ull;
+}
+// the same of the wavefronts' lists
 __device__ inline uint64_t join_lists(Shared &sh, const List &list, uint32_t n) {
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-  if (lane < VL_MAX_TOP) sh.list[wave][lane] = lane < n ? list.key : 0ull;
+  if (lane < n) sh.list[wave * n + lane] = list.key;
+  if (threadIdx.x < n) sh.key[threadIdx.x] = 0;   // (done with by now)
   __syncthreads();
-  uint64_t *out = sh.key;   // (done with by now)
-  if (threadIdx.x < kWaves * VL_MAX_TOP) {
-    const uint64_t mine = (&sh.list[0][0])[threadIdx.x];
-    uint32_t rank = 0, some = 0;
-    for (uint32_t w = 0; w < kWaves; ++w)
-      for (uint32_t k = 0; k < n; ++k) {
-        const uint64_t other = sh.list[w][k];
-        rank += other > mine;
-        some += other != 0;
-      }
-    if (mine && rank < n) out[rank] = mine;
-    if (threadIdx.x < n && threadIdx.x >= some) out[threadIdx.x] = 0;
+  return in_order(sh.list, kWaves * n, sh.key, n);
+}
+// The lowest key that is of interest when `mine` is a thread's best: what the n best of the threads' reach
+template <class T>
+__device__ inline uint64_t least_of_interest(Shared &sh, uint64_t mine, uint32_t place_bits, uint32_t n) {
+  const uint32_t lane = threadIdx.x & 63u;
+  sh.key[threadIdx.x] = mine;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    uint64_t k[kWaves];
+#pragma unroll
+    for (uint32_t i = 0; i < kWaves; ++i) k[i] = sh.key[lane + 64 * i];
+    const uint64_t least = nth_key<T::kBits, kWaves>(k, place_bits, n, n + kMoreHot);
+    uint32_t n_hot = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kWaves; ++i) {
+      const uint64_t is = __ballot(k[i] >= least);
+      if (k[i] >= least) sh.hot[n_hot + __popcll(is & ((1ull << lane) - 1ull))] = lane + 64 * i;
+      n_hot += __popcll(is);
+    }
+    if (lane == 0) {
+      sh.least = least;
+      sh.n_hot = n_hot;
+      sh.room.n = 0;
+    }
   }
   __syncthreads();
-  return threadIdx.x < n ? out[threadIdx.x] : 0ull;
+  return sh.least;
 }
 
 __device__ inline Sums join_sums(Shared &sh, Sums mine, float scale2) {
@@ -444,46 +526,41 @@ __global__ __launch_bounds__(kThreads) void k_scores_long(Rows a, Scores out, ui
     if (!parts) f = finish(a, out, r, sums, given, threadIdx.x == 0);
     else if (threadIdx.x == 0) parts[(uint64_t)r * gridDim.x + blockIdx.x] = Part{sums.m, sums.s, sums.y, 0.0f};
     if (n_top) {
-      const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-      sh.key[threadIdx.x] = mine == kNoLogit ? 0ull : key_of(ordered(mine), place);
-      __syncthreads();
-      if (wave == 0) {
-        uint64_t k[kWaves];
-#pragma unroll
-        for (uint32_t i = 0; i < kWaves; ++i) k[i] = sh.key[lane + 64 * i];
-        const uint64_t least = nth_key<kWaves>(k, n_top);
-        uint32_t n_hot = 0;
-#pragma unroll
-        for (uint32_t i = 0; i < kWaves; ++i) {
-          const uint64_t is = __ballot(k[i] >= least);
-          if (k[i] >= least) sh.hot[n_hot + __popcll(is & ((1ull << lane) - 1ull))] = lane + 64 * i;
-          n_hot += __popcll(is);
-        }
-        if (lane == 0) {
-          sh.least = least;
-          sh.n_hot = n_hot;
-        }
+      const uint64_t least = least_of_interest<T>(sh, mine == kNoLogit ? 0ull : key_of(ordered<T>(mine), place), bits_for(n_chunk), n_top);
+      // the hot lanes' chunks, dealt out to all threads
+      const uint32_t n_hot = sh.n_hot, each = (c1 - c0 + kThreads - 1) / kThreads;
+      for (uint32_t i = threadIdx.x; i < n_hot * each; i += kThreads) {
+        const uint32_t turn = i / n_hot, at = c0 + sh.hot[i - turn * n_hot] + turn * kThreads;
+        if (at >= c1) continue;
+        float x[T::kElems];
+        load_any<T>(a, row, mask, at, x);
+        each_candidate<T>(x, at, least, [&](uint64_t k, bool is) { if (is) gather(sh.room, k); });
       }
       __syncthreads();
-      List list;
-      const uint64_t least = sh.least;
-      for (uint32_t h = wave; h < sh.n_hot; h += kWaves) {
-        const uint32_t from = c0 + sh.hot[h];
-        for (uint32_t base = from; base < c1; base += 64 * kThreads) {
-          const uint32_t at = base + lane * kThreads;
-          float x[T::kElems];
-          if (at < c1) {
-            load_any<T>(a, row, mask, at, x);
-          } else {
+      uint64_t best;
+      if (sh.room.n <= kRoom) {
+        best = in_order(sh.room.key, sh.room.n, sh.key, n_top);
+      } else {
+        const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        List list;
+        for (uint32_t h = wave; h < n_hot; h += kWaves) {
+          const uint32_t from = c0 + sh.hot[h];
+          for (uint32_t base = from; base < c1; base += 64 * kThreads) {
+            const uint32_t at = base + lane * kThreads;
+            float x[T::kElems];
+            if (at < c1) {
+              load_any<T>(a, row, mask, at, x);
+            } else {
 #pragma unroll
-            for (uint32_t j = 0; j < T::kElems; ++j) x[j] = kNoLogit;
+              for (uint32_t j = 0; j < T::kElems; ++j) x[j] = kNoLogit;
+            }
+            each_candidate<T>(x, at, least, [&](uint64_t k, bool is) { list.insert_lanes(k, is, n_top); });
           }
-          list_chunk<T>(list, x, at, least, n_top);
         }
+        best = join_lists(sh, list, n_top);
       }
-      const uint64_t best = join_lists(sh, list, n_top);
       if (threadIdx.x < n_top) {
-        if (!parts) write_top(out, r, threadIdx.x, best, f);
+        if (!parts) write_top<T>(out, r, threadIdx.x, best, f);
         else part_keys[((uint64_t)r * gridDim.x + blockIdx.x) * n_top + threadIdx.x] = best;
       }
     }
@@ -511,14 +588,29 @@ __global__ __launch_bounds__(kThreads) void k_scores_join(Rows a, Scores out, ui
     sums = join_sums(sh, sums, a.scale2);
     const Final f = finish(a, out, r, sums, given, threadIdx.x == 0);
     if (n_top) {
-      List list;
+      // every thread's best of the parts' keys, then those that n of these reach
       const uint64_t VL_GLOBAL *keys = part_keys + (uint64_t)r * n_part * n_top;
-      for (uint32_t p = wave; p < n_part; p += kWaves) {
-        const uint64_t k = lane < n_top ? keys[(uint64_t)p * n_top + lane] : 0ull;
-        list.insert_lanes(k, k > list.worst, n_top);
+      uint64_t mine = 0;
+      for (uint32_t i = threadIdx.x; i < n_part * n_top; i += kThreads) mine = keys[i] > mine ? keys[i] : mine;
+      const uint64_t least = least_of_interest<T>(sh, mine, bits_for(a.n_vocab), n_top);
+      for (uint32_t i = threadIdx.x; i < n_part * n_top; i += kThreads) {
+        const uint64_t k = keys[i];
+        if (k >= least) gather(sh.room, k);
       }
-      const uint64_t best = join_lists(sh, list, n_top);
-      if (threadIdx.x < n_top) write_top(out, r, threadIdx.x, best, f);
+      __syncthreads();
+      // (at most n_top + kMoreHot threads have such keys, with VL_MAX_TOP each at most; a part's keys are next to each other)
+      uint64_t best;
+      if (sh.room.n <= kRoom) {
+        best = in_order(sh.room.key, sh.room.n, sh.key, n_top);
+      } else {
+        List list;
+        for (uint32_t p = wave; p < n_part; p += kWaves) {
+          const uint64_t k = lane < n_top ? keys[(uint64_t)p * n_top + lane] : 0ull;
+          list.insert_lanes(k, k >= least, n_top);
+        }
+        best = join_lists(sh, list, n_top);
+      }
+      if (threadIdx.x < n_top) write_top<T>(out, r, threadIdx.x, best, f);
     }
     __syncthreads();
   }

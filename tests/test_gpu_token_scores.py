@@ -236,6 +236,27 @@ def test_alternatives_among_equal_logits(n, v, top):
         check_all(y, None, top=top, what=f"distance {step}")
 
 
+@pytest.mark.parametrize("v", [512, 4096, 32768, 131072, 1 << 20])
+@pytest.mark.parametrize("top", [1, 8, 20, 32])
+def test_alternatives_that_stand_together(v, top):
+    """the best logits of a row in few of the places that are looked at together: 8 tokens in a row, such eights 512 or 2,048 tokens
+    apart, and the first 32 tokens of every eighth 4,096"""
+    t = torch.arange(v)
+    rows = []
+    for lanes in (64, 256):
+        lane, turn = t // 8 % lanes, t // (8 * lanes)
+        rows.append(torch.where(lane < 12, 200 - 8 * lane + turn % 8, 0))   # one lane's all above the next one's
+        rows.append(torch.where(lane < 12, 100 + 8 * lane - turn % 8, 0))
+    rows.append(torch.where((t // 4096 % 8 == 0) & (t % 4096 < 32), 200 - t % 4096, 0))
+    rows.append(-(t // 8) % 200)
+    x = torch.stack(rows).float()
+    for dtype in (BF16, F32):   # (every value is exact in either)
+        for n in (1, len(rows)):
+            y = x[:n] if n > 1 else x[4:5]
+            out = scores(y.to(dtype).cuda(), None, top=top)
+            check_scores(out, Rows(y, None, top=top))
+
+
 def test_outputs_that_are_not_asked_for():
     n, v = 6, 700
     x, t = bell(n, v, F16, 1), tokens(n, v, 2)
