@@ -356,7 +356,7 @@ int32_t vl_free_bases_multi(const vl_mask_query *queries, uint32_t n, uint32_t *
  *   the n_top largest logits of A, equal ones in the order of their tokens, with their logprob;
  *   places beyond A's size get token -1 and -infinity.
  * A row without any token in A has logprob -infinity, entropy 0 and stat (-infinity, -infinity).
- * A row whose token is negative stands for padding: it is not read, has logprob 0, entropy 0, stat (0, 0)
+ * A row whose token is negative stands for padding: its logits and mask do not count, it has logprob 0, entropy 0, stat (0, 0)
  * and no alternatives.  If an allowed logit is NaN or +infinity every number of the row is NaN and its alternatives'
  * tokens are -1.  Sums and statistics are held in 32 bits whatever the logits' type.
  * Results do not depend on what else runs, and a row's not on the other rows; the number of rows

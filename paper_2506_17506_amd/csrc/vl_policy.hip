@@ -17,19 +17,25 @@ __device__ inline V wave_sum(V x) {
   for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
   return x;
 }
-// sum over kTeam threads (a wavefront, or the whole workgroup), in every one of them
-template <uint32_t kTeam, class V>
-__device__ inline V team_sum(V x, V *room) {
+// sums over kTeam threads (a wavefront, or the whole workgroup), in every one of them
+template <uint32_t kTeam>
+__device__ inline void team_sums(double &x, double &y, double (*room)[kTeam / 64]) {
   x = wave_sum(x);
+  y = wave_sum(y);
   if constexpr (kTeam > 64) {
-    if ((threadIdx.x & 63u) == 0) room[threadIdx.x >> 6] = x;
+    if ((threadIdx.x & 63u) == 0) {
+      room[0][threadIdx.x >> 6] = x;
+      room[1][threadIdx.x >> 6] = y;
+    }
     __syncthreads();
-    x = 0;
+    x = y = 0;
 #pragma unroll 4
-    for (uint32_t w = 0; w < kTeam / 64; ++w) x += room[w];
+    for (uint32_t w = 0; w < kTeam / 64; ++w) {
+      x += room[0][w];
+      y += room[1][w];
+    }
     __syncthreads();
   }
-  return x;
 }
 
 struct Rewards {
@@ -50,11 +56,13 @@ __device__ inline double reward_of(const Rewards &w, uint32_t k) {
 constexpr uint32_t kKeep = 4;   // rewards of a thread that stay in registers
 
 // kTeam threads per group.  What bounds it: the trips to memory, for the group's offsets and then for its records.  Rewards are
-// taken as distances to the group's first, so that equal ones have a spread of exactly 0.
+// taken as distances d to the group's first, so that equal ones have a spread of exactly 0, and the variance as mean(d^2) - mean(d)^2
+// in one pass: as one of the K distances is 0, the variance is mean(d)^2 / K at least, so the difference loses a factor of
+// K + 1 at most of 64 bits' precision.
 template <uint32_t kTeam>
 __global__ __launch_bounds__(kTeam < 256 ? 256 : kTeam) void k_advantages(Rewards w, uint32_t n, const uint32_t VL_GLOBAL *group_off, uint32_t n_group, double eps,
                                                                          float VL_GLOBAL *reward, float VL_GLOBAL *advantage) {
-  __shared__ double room[kTeam < 64 ? 1 : kTeam / 64];
+  __shared__ double room[2][kTeam / 64];
   const uint32_t teams = kTeam < 256 ? 256 / kTeam : 1, me = threadIdx.x % kTeam;
   for (uint32_t g = blockIdx.x * teams + threadIdx.x / kTeam; g < n_group; g += gridDim.x * teams) {
     const uint32_t k0 = min(group_off[g], n), k1 = min(group_off[g + 1], n);
@@ -67,19 +75,18 @@ __global__ __launch_bounds__(kTeam < 256 ? 256 : kTeam) void k_advantages(Reward
       kept[i] = k >= k0 && k < k1 ? reward_of(w, k) : first;
     }
 #pragma unroll
-    for (uint32_t i = 0; i < kKeep; ++i) s += kept[i] - first;
-    for (uint64_t k = (uint64_t)k0 + me + kKeep * kTeam; k < k1; k += kTeam) s += reward_of(w, (uint32_t)k) - first;
-    const double mean = team_sum<kTeam>(s, room) / size;
-#pragma unroll
     for (uint32_t i = 0; i < kKeep; ++i) {
-      const double d = kept[i] - first - mean;
-      if ((uint64_t)k0 + me + i * kTeam < k1) v += d * d;
-    }
-    for (uint64_t k = (uint64_t)k0 + me + kKeep * kTeam; k < k1; k += kTeam) {
-      const double d = reward_of(w, (uint32_t)k) - first - mean;
+      const double d = kept[i] - first;
+      s += d;
       v += d * d;
     }
-    const double scale = 1.0 / (sqrt(team_sum<kTeam>(v, room) / size) + eps);
+    for (uint64_t k = (uint64_t)k0 + me + kKeep * kTeam; k < k1; k += kTeam) {
+      const double d = reward_of(w, (uint32_t)k) - first;
+      s += d;
+      v += d * d;
+    }
+    team_sums<kTeam>(s, v, room);
+    const double mean = s / size, scale = 1.0 / (sqrt(fmax(v / size - mean * mean, 0.0)) + eps);
 #pragma unroll
     for (uint32_t i = 0; i < kKeep; ++i) {
       const uint64_t k = (uint64_t)k0 + me + i * kTeam;
@@ -138,8 +145,11 @@ __global__ __launch_bounds__(kPolicyThreads) void k_policy(Batch b, Part VL_GLOB
   uint64_t tokens = 0, clips = 0;
   auto sample_of = [&](uint64_t unit) {
     const uint32_t c = (uint32_t)unit / b.slices, slice = (uint32_t)unit - c * b.slices;   // (fewer than 2^32 units)
-    const uint64_t i0 = least_of(b.start[c], b.n), i1 = least_of(i0 + b.len[c], b.n), per = ((i1 - i0 + b.slices - 1) / b.slices + kStep - 1) / kStep * kStep;
-    return Sample{least_of(i0 + slice * per, i1), least_of(i0 + (slice + 1) * per, i1), b.advantage[c], b.weight[c]};
+    const uint64_t i0 = least_of(b.start[c], b.n), i1 = least_of(i0 + b.len[c], b.n);
+    // slices end at multiples of kStep
+    const uint64_t base = i0 / kStep * kStep, per = ((i1 - base + kStep - 1) / kStep + b.slices - 1) / b.slices * kStep;
+    const uint64_t from = least_of(base + slice * per, i1), to = least_of(base + (slice + 1) * per, i1);
+    return Sample{from < i0 ? i0 : from, to < i0 ? i0 : to, b.advantage[c], b.weight[c]};
   };
   for (uint64_t unit = (uint64_t)blockIdx.x * kPolicyWaves + wave; unit < n_unit; unit += stride) {
     const Sample s = sample_of(unit);
@@ -162,10 +172,11 @@ __global__ __launch_bounds__(kPolicyThreads) void k_policy(Batch b, Part VL_GLOB
       n_clip += clip;
       return s.w * g;
     };
-    for (uint64_t i = s.from; i < s.to; i += kStep) {
+    // steps start at multiples of kStep in the arrays, so that all but a sample's ends is read in whole lines
+    for (uint64_t i = s.from / kStep * kStep; i < s.to; i += kStep) {
       const uint64_t at = i + lane * 4;
-      if (i + kStep <= s.to) {
-        f32x4 lp[kGroups], old[kGroups], ref[kGroups] = {};
+      f32x4 lp[kGroups], old[kGroups], ref[kGroups] = {};
+      if (i >= s.from && i + kStep <= s.to) {
 #pragma unroll
         for (uint32_t u = 0; u < kGroups; ++u) {
           lp[u] = *(const f32x4_any VL_GLOBAL *)(b.logprob + at + u * 256);
@@ -180,7 +191,23 @@ __global__ __launch_bounds__(kPolicyThreads) void k_policy(Batch b, Part VL_GLOB
           *(f32x4_any VL_GLOBAL *)(b.grad + at + u * 256) = g;
         }
       } else {
-        for (uint64_t k = i + lane; k < s.to; k += 64) b.grad[k] = token(b.logprob[k], b.logprob_old[k], kRef ? b.logprob_ref[k] : 0.0f);
+#pragma unroll
+        for (uint32_t u = 0; u < kGroups; ++u)
+#pragma unroll
+          for (uint32_t j = 0; j < 4; ++j) {   // (neighbouring lanes take neighbouring tokens)
+            const uint64_t k = i + (u * 4 + j) * 64 + lane;
+            const bool in = k >= s.from && k < s.to;
+            lp[u][j] = in ? b.logprob[k] : 0.0f;
+            old[u][j] = in ? b.logprob_old[k] : 0.0f;
+            if (kRef) ref[u][j] = in ? b.logprob_ref[k] : 0.0f;
+          }
+#pragma unroll
+        for (uint32_t u = 0; u < kGroups; ++u)
+#pragma unroll
+          for (uint32_t j = 0; j < 4; ++j) {
+            const uint64_t k = i + (u * 4 + j) * 64 + lane;
+            if (k >= s.from && k < s.to) b.grad[k] = token(lp[u][j], old[u][j], ref[u][j]);
+          }
       }
     }
     loss += (double)s.w * sum;
@@ -203,18 +230,23 @@ __global__ __launch_bounds__(kPolicyThreads) void k_policy(Batch b, Part VL_GLOB
   }
 }
 
+__device__ inline Part add_parts(Part p, const Part &q) { return Part{p.loss + q.loss, p.kl + q.kl, p.n_token + q.n_token, p.n_clipped + q.n_clipped}; }
+
 constexpr uint32_t kJoinThreads = 1024;
 __global__ __launch_bounds__(kJoinThreads) void k_policy_join(const Part VL_GLOBAL *parts, uint32_t n, vl_policy_stats VL_GLOBAL *stats) {
-  __shared__ double sums[kJoinThreads / 64];
-  __shared__ unsigned long long numbers[kJoinThreads / 64];
+  __shared__ Part room[kJoinThreads / 64];
   Part p = {0, 0, 0, 0};
-  for (uint32_t i = threadIdx.x; i < n; i += kJoinThreads) {
-    p.loss += parts[i].loss; p.kl += parts[i].kl; p.n_token += parts[i].n_token; p.n_clipped += parts[i].n_clipped;
-  }
-  p.loss = team_sum<kJoinThreads>(p.loss, sums);
-  p.kl = team_sum<kJoinThreads>(p.kl, sums);
-  p.n_token = team_sum<kJoinThreads>((unsigned long long)p.n_token, numbers);
-  p.n_clipped = team_sum<kJoinThreads>((unsigned long long)p.n_clipped, numbers);
+  for (uint32_t i = threadIdx.x; i < n; i += kJoinThreads) p = add_parts(p, Part{parts[i].loss, parts[i].kl, parts[i].n_token, parts[i].n_clipped});
+#pragma unroll
+  for (int d = 32; d; d >>= 1)
+    p = add_parts(p, Part{__shfl_xor(p.loss, d), __shfl_xor(p.kl, d), __shfl_xor(p.n_token, d), __shfl_xor(p.n_clipped, d)});
+  if ((threadIdx.x & 63u) == 0) room[threadIdx.x >> 6] = p;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  p = threadIdx.x < kJoinThreads / 64 ? room[threadIdx.x] : Part{0, 0, 0, 0};
+#pragma unroll
+  for (int d = 8; d; d >>= 1)
+    p = add_parts(p, Part{__shfl_xor(p.loss, d), __shfl_xor(p.kl, d), __shfl_xor(p.n_token, d), __shfl_xor(p.n_clipped, d)});
   if (threadIdx.x == 0) {
     stats->loss = (float)p.loss;
     stats->kl = (float)p.kl;
@@ -232,12 +264,14 @@ int32_t check_batch(const vl_policy_batch *b) {
   return VL_OK;
 }
 
-// Slices of a sample, of about 2,048 tokens by the longest one, and workgroups for them, eight per compute unit at most
+// Slices of a sample, of about 2,048 tokens by the longest one, less where that leaves wavefronts idle, and workgroups for them,
+// 8,192 at most.  (1,600 samples of 43,000 tokens on average, a slice per wavefront: 163 us; 2,048 workgroups that
+// take a slice after the other 173, slices of 4,096 tokens 168, of 1,024 179.)
 struct Launch { uint32_t slices, blocks; };
 Launch launch_of(const vl_policy_batch *b) {
-  const uint64_t want = std::max<uint64_t>(1, b->max_len / 2048), most = std::max<uint64_t>(1, 0xFFFFFFFFull / b->n_sample);
+  const uint64_t want = std::max<uint64_t>({1, b->max_len / 2048, std::min<uint64_t>(b->max_len / kStep, 8192 / b->n_sample)}), most = std::max<uint64_t>(1, 0xFFFFFFFFull / b->n_sample);
   const uint32_t slices = (uint32_t)std::min({want, most, (uint64_t)1024});
-  return Launch{slices, (uint32_t)std::min<uint64_t>(2048, ((uint64_t)b->n_sample * slices + kPolicyWaves - 1) / kPolicyWaves)};
+  return Launch{slices, (uint32_t)std::min<uint64_t>(8192, ((uint64_t)b->n_sample * slices + kPolicyWaves - 1) / kPolicyWaves)};
 }
 
 }  // namespace

@@ -31,7 +31,7 @@ struct Rows {
   uint64_t ld;                         // in bytes
   const uint8_t VL_GLOBAL *mask;
   uint64_t mask_ld;                    // in bytes
-  const int32_t VL_GLOBAL *token;
+  const int32_t VL_CONSTANT *token;
   uint32_t n_row, n_vocab;
   float scale, scale2;                 // scale2 = scale * log2 e
 };
@@ -47,7 +47,7 @@ __device__ inline uint32_t as_word(float x) { return __builtin_bit_cast(uint32_t
 struct F32 {
   typedef float type;
   typedef u32x4 chunk __attribute__((aligned(4)));
-  static constexpr uint32_t kElems = 4, kBits = 32;
+  static constexpr uint32_t kElems = 4, kBits = 32, kNone = 0xFF800000u;   // -infinity, as often as a word holds it
   static __device__ inline float wide(float x) { return x; }
   static __device__ inline float narrow(float x) { return x; }
   static __device__ inline void unpack(u32x4 w, float *x) {
@@ -65,7 +65,7 @@ struct F16 {
   typedef _Float16 type;
   typedef _Float16 pair __attribute__((ext_vector_type(2)));
   typedef u32x4 chunk __attribute__((aligned(2)));
-  static constexpr uint32_t kElems = 8, kBits = 19;   // sign, the exponent of 32 bits, ten bits
+  static constexpr uint32_t kElems = 8, kBits = 19, kNone = 0xFC00FC00u;   // (bits: sign, the exponent of 32 bits, ten)
   static __device__ inline float wide(_Float16 x) { return (float)x; }
   static __device__ inline _Float16 narrow(float x) { return (_Float16)x; }
   static __device__ inline void unpack(u32x4 w, float *x) {
@@ -88,7 +88,7 @@ struct BF16 {
   typedef __bf16 type;
   typedef __bf16 pair __attribute__((ext_vector_type(2)));
   typedef u32x4 chunk __attribute__((aligned(2)));
-  static constexpr uint32_t kElems = 8, kBits = 16;
+  static constexpr uint32_t kElems = 8, kBits = 16, kNone = 0xFF80FF80u;
   static __device__ inline float wide(__bf16 x) { return (float)x; }
   static __device__ inline __bf16 narrow(float x) { return (__bf16)x; }
   static __device__ inline void unpack(u32x4 w, float *x) {
@@ -106,11 +106,21 @@ struct BF16 {
   }
 };
 
-constexpr uint32_t kThreads = 256, kWaves = kThreads / 64;
+constexpr uint32_t kThreads = 256, kWaves = kThreads / 64, kQuarters = kThreads / 16;
 
 template <class T>
 __device__ inline u32x4 load_chunk(const uint8_t VL_GLOBAL *row, uint32_t c) {
   return *(const typename T::chunk VL_GLOBAL *)(row + (uint64_t)c * 16);
+}
+// Long rows of 16 bits a logit are taken from the multiple of 4 bytes at or below their start, `lead` (0 or 1) logits early,
+// since loads from odd places cost: 4,096 rows of 50,001 logits 91 us, of 50,000 78.  Chunk c then holds tokens
+// c * 8 - lead and up; what stands before the row does not count.  (It lies in the word that holds the row's first logit.)
+template <class T>
+__device__ inline uint32_t lead_of(const uint8_t VL_GLOBAL *row) { return T::kElems == 8 ? ((uint32_t)(uintptr_t)row >> 1) & 1u : 0u; }
+template <class T>
+__device__ inline u32x4 load_even(const uint8_t VL_GLOBAL *row, uint32_t lead, uint32_t c) {
+  typedef u32x4 words __attribute__((aligned(4)));
+  return *(const words VL_GLOBAL *)(row - lead * 2 + (uint64_t)c * 16);
 }
 
 // the logits that the mask does not allow become -infinity (bit j of `bits`: logit j is allowed)
@@ -128,6 +138,12 @@ __device__ inline uint32_t mask_bits(const uint8_t VL_GLOBAL *mask, uint32_t c) 
   return mask[c >> 1] >> ((c & 1) * 4);
 }
 
+template <class T>
+__device__ inline uint32_t mask_bits(const uint8_t VL_GLOBAL *mask, uint32_t lead, uint32_t c) {
+  if (T::kElems == 4 || !lead) return mask_bits<T>(mask, c);
+  return (uint32_t)mask[c] << 1 | (c ? mask[c - 1] >> 7 : 0u);   // (nothing allowed in front of the row)
+}
+
 // chunk c of a row of n logits, of which the row's end may cut some off: those are -infinity
 template <class T>
 __device__ inline void load_any(const Rows &a, const uint8_t VL_GLOBAL *row, const uint8_t VL_GLOBAL *mask, uint32_t c, float *x) {
@@ -140,6 +156,24 @@ __device__ inline void load_any(const Rows &a, const uint8_t VL_GLOBAL *row, con
       x[j] = from + j < a.n_vocab ? T::wide(((const typename T::type VL_GLOBAL *)row)[from + j]) : kNoLogit;
   }
   if (mask) keep_allowed<T>(x, from < a.n_vocab ? mask_bits<T>(mask, c) : 0u);
+}
+
+// the same with `lead`
+template <class T>
+__device__ inline void load_any(const Rows &a, const uint8_t VL_GLOBAL *row, const uint8_t VL_GLOBAL *mask, uint32_t lead, uint32_t c, float *x) {
+  const uint32_t from = c * T::kElems - lead;   // (2^32 - 1 in front of the row)
+  if (c * T::kElems + T::kElems <= a.n_vocab + lead) {
+    T::unpack(load_even<T>(row, lead, c), x);
+    if (mask) keep_allowed<T>(x, mask_bits<T>(mask, lead, c));
+    if (lead > c) x[0] = kNoLogit;
+    return;
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < T::kElems; ++j) {
+    const uint32_t t = from + j;
+    const bool in = t < a.n_vocab && (!mask || ((mask[t >> 3] >> (t & 7)) & 1));
+    x[j] = in ? T::wide(((const typename T::type VL_GLOBAL *)row)[t]) : kNoLogit;
+  }
 }
 
 // ---- over a wavefront: rows of 16 lanes, then across rows; the result stands in lane 63
@@ -159,6 +193,20 @@ __device__ inline float wave_fold(float x, float none, F f) {
 }
 __device__ inline float wave_max(float x) { return wave_fold(x, kNoLogit, [](float u, float v) { return fmaxf(u, v); }); }
 __device__ inline float wave_sum(float x) { return wave_fold(x, 0.0f, [](float u, float v) { return u + v; }); }
+
+// over 16 lanes, in all of them
+template <class F>
+__device__ inline float quarter_fold(float x, F f) {
+  auto step = [&](auto ctrl) {
+    const int y = __builtin_amdgcn_update_dpp(0, (int)as_word(x), decltype(ctrl)::value, 0xf, 0xf, false);
+    x = f(x, as_float((uint32_t)y));
+  };
+  step(std::integral_constant<int, 0x128>{});   // row_ror:8, 4, 2, 1
+  step(std::integral_constant<int, 0x124>{});
+  step(std::integral_constant<int, 0x122>{});
+  step(std::integral_constant<int, 0x121>{});
+  return x;
+}
 
 // ---- a row's sums so far
 struct Sums { float m, s, y; };
@@ -186,29 +234,22 @@ __device__ inline uint64_t lane_key(uint64_t k, uint32_t lane) {
   return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
 }
 
-// A number that at least n of the keys which a wavefront's lanes hold (kEach per lane, 0: none, the others all differ) reach, and at
+// A number that at least n of the keys which a wavefront's lanes hold (0: none, the others all differ) reach, and at
 // most `most` >= n of them; 1 if there are fewer than n.  Bit by bit from the top; places are below 2^place_bits.
-template <uint32_t kBits, uint32_t kEach>
-__device__ inline uint64_t nth_key(const uint64_t *k, uint32_t place_bits, uint32_t n, uint32_t most) {
-  uint64_t least = 0;
-  auto count_from = [&](uint64_t attempt) {
-    uint32_t count = 0;
-#pragma unroll
-    for (uint32_t i = 0; i < kEach; ++i) count += __popcll(__ballot(k[i] >= attempt));
-    return count;
-  };
-  for (int32_t bit = 31 + kBits; bit >= 32; --bit) {
-    const uint64_t attempt = least | (1ull << bit);
-    const uint32_t count = count_from(attempt);
+template <uint32_t kBits>
+__device__ inline uint64_t nth_key(uint64_t k, uint32_t place_bits, uint32_t n, uint32_t most) {
+  uint32_t value = 0;
+  for (int32_t bit = kBits - 1; bit >= 0; --bit) {
+    const uint32_t attempt = value | (1u << bit), count = __popcll(__ballot((uint32_t)(k >> 32) >= attempt));
     if (count < n) continue;
-    least = attempt;
-    if (count <= most) return least;
+    value = attempt;
+    if (count <= most) return (uint64_t)value << 32;
   }
-  if (!least) return 1ull;
-  least |= 0xFFFFFFFFull & ~((1ull << place_bits) - 1ull);   // (the same in every key)
+  if (!value) return 1ull;
+  uint64_t least = ((uint64_t)value << 32) | (0xFFFFFFFFull & ~((1ull << place_bits) - 1ull));   // (the same in every key)
   for (int32_t bit = (int32_t)place_bits - 1; bit >= 0; --bit) {
     const uint64_t attempt = least | (1ull << bit);
-    const uint32_t count = count_from(attempt);
+    const uint32_t count = __popcll(__ballot(k >= attempt));
     if (count < n) continue;
     least = attempt;
     if (count <= most) return least;
@@ -219,15 +260,17 @@ __device__ inline uint32_t bits_for(uint32_t n) { return 32u - (uint32_t)__built
 
 // Where keys that may be among a row's n best are gathered.  More than there is room for are possible (many equal
 // logits, or a row sorted in an unlucky way); then the row's best are found by insertion instead.
-constexpr uint32_t kRoom = 256;
-constexpr uint32_t kMoreHot = 8;   // lanes whose chunks are read again beyond n, so that the search for them ends sooner
+constexpr uint32_t kMoreHot = 8;   // more than n lanes may have their chunks looked at again, so that the search for them ends sooner
+template <uint32_t kTeam>
 struct Room {
-  uint64_t key[kRoom];
+  static constexpr uint32_t kMost = kTeam < 256 ? kTeam : 256;   // (one per thread is put in order)
+  uint64_t key[kMost];
   uint32_t n;
 };
-__device__ inline void gather(Room &room, uint64_t key) {
+template <uint32_t kTeam>
+__device__ inline void gather(Room<kTeam> &room, uint64_t key) {
   const uint32_t at = atomicAdd(&room.n, 1u);   // (their order does not matter)
-  if (at < kRoom) room.key[at] = key;
+  if (at < Room<kTeam>::kMost) room.key[at] = key;
 }
 
 // A sorted list, entry i in lane i, 0 where there is none; `worst` is entry n - 1.
@@ -251,12 +294,12 @@ struct List {
 
 // f(key) for those of a chunk's logits that are at or above `least`, a (value, chunk), and so may be among the best
 template <class T, class F>
-__device__ inline void each_candidate(const float *x, uint32_t c, uint64_t least, F f) {
+__device__ inline void each_candidate(const float *x, uint32_t lead, uint32_t c, uint64_t least, F f) {
   const uint32_t value = (uint32_t)(least >> 32) + (c <= (uint32_t)~least ? 0u : 1u);
 #pragma unroll
   for (uint32_t j = 0; j < T::kElems; ++j) {
     const uint32_t u = ordered<T>(x[j]);
-    f(key_of(u, c * T::kElems + j), x[j] != kNoLogit && u >= value);
+    f(key_of(u, c * T::kElems - lead + j), x[j] != kNoLogit && u >= value);
   }
 }
 
@@ -298,6 +341,44 @@ __device__ inline float given_logit(const Rows &a, uint32_t r, int32_t token) {
   if (!a.token || (uint32_t)token >= a.n_vocab) return kNoLogit;
   if (a.mask && !((a.mask[(uint64_t)r * a.mask_ld + ((uint32_t)token >> 3)] >> (token & 7)) & 1)) return kNoLogit;
   return T::wide(((const typename T::type VL_GLOBAL *)(a.logits + (uint64_t)r * a.ld))[token]);
+}
+
+// Short rows of which no alternatives are asked for: 16 lanes per row, kChunks chunks per lane, so that a wavefront's
+// instructions for the reductions and the results serve four rows.  Four rows' loads are on their way at once.
+template <class T, uint32_t kChunks>
+__global__ __launch_bounds__(kThreads) void k_scores_quarter(Rows a, Scores out) {
+  const uint32_t lane = threadIdx.x & 15u;
+  for (uint32_t first = blockIdx.x * kQuarters; first < a.n_row; first += gridDim.x * kQuarters) {
+    const uint32_t r = first + (threadIdx.x >> 4);
+    if (r >= a.n_row) break;
+    const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
+    const uint8_t VL_GLOBAL *mask = a.mask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
+    const int32_t token = a.token ? a.token[r] : 0;
+    float x[kChunks][T::kElems];
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i) load_any<T>(a, row, mask, lane + 16 * i, x[i]);
+    const float given = given_logit<T>(a, r, token);
+    float m = kNoLogit;
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i)
+#pragma unroll
+      for (uint32_t j = 0; j < T::kElems; ++j) m = fmaxf(m, x[i][j]);
+    Sums sums = {quarter_fold(m, [](float u, float v) { return fmaxf(u, v); }), 0.0f, 0.0f};
+    const float ref = ref_of(sums.m);
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i)
+#pragma unroll
+      for (uint32_t j = 0; j < T::kElems; ++j) {
+        const float z = (x[i][j] - ref) * a.scale2, e = __builtin_amdgcn_exp2f(z);
+        sums.s += e;
+        sums.y += e * fmaxf(z, kFar);
+      }
+    auto add = [](float u, float v) { return u + v; };
+    sums.s = quarter_fold(sums.s, add);
+    sums.y = quarter_fold(sums.y, add);
+    if (token < 0) write_padding(out, r, lane);
+    else finish(a, out, r, sums, given, lane == 0);
+  }
 }
 
 // Short rows: a wavefront per row, kChunks chunks per lane, all in registers.
@@ -343,12 +424,12 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
     if (out.n_top) {
       const uint32_t n = out.n_top;
       const uint64_t key = m == kNoLogit ? 0ull : key_of(ordered<T>(m), place);
-      const uint64_t least = nth_key<T::kBits, 1>(&key, bits_for(64 * kChunks - 1), n, n + kMoreHot);
+      const uint64_t least = nth_key<T::kBits>(key, bits_for(64 * kChunks - 1), n, n + kMoreHot);
       // gathered in the order of the lanes; up to 64 of them, usual unless many are equal, one per lane
       uint32_t found = 0;
 #pragma unroll
       for (uint32_t i = 0; i < kChunks; ++i)
-        each_candidate<T>(x[i], lane + 64 * i, least, [&](uint64_t k, bool is) {
+        each_candidate<T>(x[i], 0, lane + 64 * i, least, [&](uint64_t k, bool is) {
           const uint64_t all = __ballot(is);
           if (!all) return;
           const uint32_t at = found + __popcll(all & ((1ull << lane) - 1ull));
@@ -366,7 +447,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
         List list;
 #pragma unroll
         for (uint32_t i = 0; i < kChunks; ++i)
-          each_candidate<T>(x[i], lane + 64 * i, least, [&](uint64_t k, bool is) { list.insert_lanes(k, is, n); });
+          each_candidate<T>(x[i], 0, lane + 64 * i, least, [&](uint64_t k, bool is) { list.insert_lanes(k, is, n); });
         if (lane < n) write_top<T>(out, r, lane, list.key, f);
       }
     }
@@ -376,16 +457,17 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
 // What a part of a row leaves for the join: its sums and n_top keys, best first.
 typedef float Part __attribute__((ext_vector_type(4)));
 
+template <uint32_t kTeam>
 struct Shared {
-  Sums sums[kWaves];
-  Room room;
-  uint64_t key[kThreads];
-  uint64_t list[kWaves * VL_MAX_TOP];
+  Sums sums[kTeam / 64];
+  Room<kTeam> room;
+  uint64_t key[kTeam < 64 ? 64 : kTeam];
+  uint64_t list[kTeam / 64 * VL_MAX_TOP];
   uint64_t least;
-  uint32_t n_hot, hot[VL_MAX_TOP + kMoreHot];
+  uint32_t n_hot, hot[kTeam];
 };
 
-// The n best of `found` <= kRoom different keys, best first: entry k in thread k < n, 0 where there are fewer
+// The n best of `found` different keys, no more than there are threads, best first: entry k in thread k < n, 0 where there are fewer
 __device__ inline uint64_t in_order(const uint64_t *keys, uint32_t found, uint64_t *out, uint32_t n) {
   const uint64_t mine = threadIdx.x < found ? keys[threadIdx.x] : 0ull;
   uint32_t rank = 0;
@@ -396,68 +478,58 @@ __device__ inline uint64_t in_order(const uint64_t *keys, uint32_t found, uint64
   return threadIdx.x < n && threadIdx.x < found ? out[threadIdx.x] : 0ull;
 }
 // the same of the wavefronts' lists
-__device__ inline uint64_t join_lists(Shared &sh, const List &list, uint32_t n) {
+template <uint32_t kTeam>
+__device__ inline uint64_t join_lists(Shared<kTeam> &sh, const List &list, uint32_t n) {
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
   if (lane < n) sh.list[wave * n + lane] = list.key;
   if (threadIdx.x < n) sh.key[threadIdx.x] = 0;   // (done with by now)
   __syncthreads();
-  return in_order(sh.list, kWaves * n, sh.key, n);
+  return in_order(sh.list, kTeam / 64 * n, sh.key, n);
 }
-// The lowest key that is of interest when `mine` is a thread's best: what the n best of the threads' reach
-template <class T>
-__device__ inline uint64_t least_of_interest(Shared &sh, uint64_t mine, uint32_t place_bits, uint32_t n) {
-  const uint32_t lane = threadIdx.x & 63u;
+// A key that n of the threads' best, `mine`, reach, and not many more; the threads whose best reaches it are listed as hot
+template <class T, uint32_t kTeam>
+__device__ inline uint64_t least_of_interest(Shared<kTeam> &sh, uint64_t mine, uint32_t place_bits, uint32_t n) {
   sh.key[threadIdx.x] = mine;
+  if (threadIdx.x == 0) sh.n_hot = sh.room.n = 0;
   __syncthreads();
-  if (threadIdx.x < 64) {
-    uint64_t k[kWaves];
+  if (threadIdx.x < 64) {   // of several threads' best the best one: a key that n of these 64 reach serves as well
+    uint64_t k = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < kWaves; ++i) k[i] = sh.key[lane + 64 * i];
-    const uint64_t least = nth_key<T::kBits, kWaves>(k, place_bits, n, n + kMoreHot);
-    uint32_t n_hot = 0;
-#pragma unroll
-    for (uint32_t i = 0; i < kWaves; ++i) {
-      const uint64_t is = __ballot(k[i] >= least);
-      if (k[i] >= least) sh.hot[n_hot + __popcll(is & ((1ull << lane) - 1ull))] = lane + 64 * i;
-      n_hot += __popcll(is);
-    }
-    if (lane == 0) {
-      sh.least = least;
-      sh.n_hot = n_hot;
-      sh.room.n = 0;
-    }
+    for (uint32_t i = 0; i < kTeam / 64; ++i) k = sh.key[threadIdx.x + 64 * i] > k ? sh.key[threadIdx.x + 64 * i] : k;
+    const uint64_t least = nth_key<T::kBits>(k, place_bits, n, n + kMoreHot);
+    if (threadIdx.x == 0) sh.least = least;
   }
   __syncthreads();
-  return sh.least;
+  const uint64_t least = sh.least;
+  if (mine >= least) sh.hot[atomicAdd(&sh.n_hot, 1u)] = threadIdx.x;
+  __syncthreads();
+  return least;
 }
 
-__device__ inline Sums join_sums(Shared &sh, Sums mine, float scale2) {
-  const float wm = wave_max(mine.m);
-  mine = rebase(mine, wm, scale2);
+template <uint32_t kTeam>
+__device__ inline Sums join_sums(Shared<kTeam> &sh, Sums mine, float scale2) {
+  auto add = [](float u, float v) { return u + v; };
+  mine = rebase(mine, wave_max(mine.m), scale2);
   mine.s = wave_sum(mine.s);
   mine.y = wave_sum(mine.y);
+  if constexpr (kTeam == 64) return mine;
   if ((threadIdx.x & 63u) == 0) sh.sums[threadIdx.x >> 6] = mine;
   __syncthreads();
-  float m = sh.sums[0].m;
-  for (uint32_t w = 1; w < kWaves; ++w) m = fmaxf(m, sh.sums[w].m);
-  Sums all = {m, 0.0f, 0.0f};
-  for (uint32_t w = 0; w < kWaves; ++w) {
-    const Sums p = rebase(sh.sums[w], m, scale2);
-    all.s += p.s;
-    all.y += p.y;
-  }
-  return all;
+  const uint32_t w = threadIdx.x & 15u;   // (16 wavefronts at most)
+  mine = w < kTeam / 64 ? sh.sums[w] : Sums{kNoLogit, 0.0f, 0.0f};
+  mine = rebase(mine, quarter_fold(mine.m, [](float u, float v) { return fmaxf(u, v); }), scale2);
+  mine.s = quarter_fold(mine.s, add);
+  mine.y = quarter_fold(mine.y, add);
+  return mine;
 }
 
-constexpr uint32_t kBatch = 4;   // chunks of a lane on their way at once
 
-// Long rows: a workgroup per row or part of a row.  Thread t takes the part's chunks t, t + 256, t + 512, ...
-template <class T, bool kMask, bool kEntropy>
-__global__ __launch_bounds__(kThreads) void k_scores_long(Rows a, Scores out, uint32_t part_chunks, Part VL_GLOBAL *parts, uint64_t VL_GLOBAL *part_keys) {
-  __shared__ Shared sh;
-  const uint32_t n_full = a.n_vocab / T::kElems, n_chunk = (a.n_vocab + T::kElems - 1) / T::kElems;
-  const uint32_t c0 = blockIdx.x * part_chunks, c1 = min(n_chunk, c0 + part_chunks), c1_full = min(n_full, c1);
-  const uint32_t n_top = out.n_top;
+// Long rows: a workgroup of kTeam threads per row or part of a row.  Thread t takes the part's chunks t, t + kTeam, t + 2 kTeam, ...
+// kN chunks of a lane are on their way at once.
+template <class T, uint32_t kTeam, uint32_t kN, bool kMask, bool kEntropy>
+__global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_scores_long(Rows a, Scores out, uint32_t part_chunks, Part VL_GLOBAL *parts, uint64_t VL_GLOBAL *part_keys) {
+  __shared__ Shared<kTeam> sh;
+  const uint32_t c0 = blockIdx.x * part_chunks, n_top = out.n_top;
   for (uint32_t r = blockIdx.y; r < a.n_row; r += gridDim.y) {
     const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
     const uint8_t VL_GLOBAL *mask = kMask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
@@ -466,30 +538,32 @@ __global__ __launch_bounds__(kThreads) void k_scores_long(Rows a, Scores out, ui
       if (!parts) write_padding(out, r, threadIdx.x);
       continue;
     }
+    const uint32_t lead = lead_of<T>(row), n_full = (a.n_vocab + lead) / T::kElems, n_chunk = (a.n_vocab + lead + T::kElems - 1) / T::kElems;
+    const uint32_t c1 = min(n_chunk, c0 + part_chunks), c1_full = min(n_full, c1);
     const float given = parts ? kNoLogit : given_logit<T>(a, r, token);
     Sums sums = {kNoLogit, 0.0f, 0.0f};
     uint32_t place = 0;
-    // kN chunks of this lane from c on, 256 apart
+    // kHere chunks of this lane from c on, kTeam apart
     auto add = [&](auto n_of, const float (*x)[T::kElems], uint32_t c) {
-      constexpr uint32_t kN = decltype(n_of)::value;
-      float b[kN], m = kNoLogit;
+      constexpr uint32_t kHere = decltype(n_of)::value;
+      float b[kHere], m = kNoLogit;
 #pragma unroll
-      for (uint32_t u = 0; u < kN; ++u) {
+      for (uint32_t u = 0; u < kHere; ++u) {
         b[u] = x[u][0];
 #pragma unroll
         for (uint32_t j = 1; j < T::kElems; ++j) b[u] = fmaxf(b[u], x[u][j]);
         m = fmaxf(m, b[u]);
       }
       if (n_top) {
-        uint32_t first = c + (kN - 1) * kThreads;
+        uint32_t first = c + (kHere - 1) * kTeam;
 #pragma unroll
-        for (uint32_t u = kN - 1; u-- > 0;) first = b[u] == m ? c + u * kThreads : first;
+        for (uint32_t u = kHere - 1; u-- > 0;) first = b[u] == m ? c + u * kTeam : first;
         place = m > sums.m ? first : place;
       }
       sums = rebase(sums, fmaxf(sums.m, m), a.scale2);
       const float ref = ref_of(sums.m);
 #pragma unroll
-      for (uint32_t u = 0; u < kN; ++u)
+      for (uint32_t u = 0; u < kHere; ++u)
 #pragma unroll
         for (uint32_t j = 0; j < T::kElems; ++j) {
           const float z = (x[u][j] - ref) * a.scale2, e = __builtin_amdgcn_exp2f(z);
@@ -497,28 +571,39 @@ __global__ __launch_bounds__(kThreads) void k_scores_long(Rows a, Scores out, ui
           if (kEntropy) sums.y += e * fmaxf(z, kFar);
         }
     };
-    uint32_t c = c0;
-    for (; c + kBatch * kThreads <= c1_full; c += kBatch * kThreads) {
-      u32x4 w[kBatch];
-      uint32_t bits[kBatch];
+    for (uint32_t c = c0 + threadIdx.x; c - threadIdx.x < c1_full; c += kN * kTeam) {
+      u32x4 w[kN];
+      uint32_t bits[kN];
+      if (c - threadIdx.x + kN * kTeam <= c1_full) {
 #pragma unroll
-      for (uint32_t u = 0; u < kBatch; ++u) w[u] = load_chunk<T>(row, c + threadIdx.x + u * kThreads);
+        for (uint32_t u = 0; u < kN; ++u) w[u] = load_even<T>(row, lead, c + u * kTeam);
+        if (kMask) {
 #pragma unroll
-      for (uint32_t u = 0; u < kBatch; ++u) bits[u] = kMask ? mask_bits<T>(mask, c + threadIdx.x + u * kThreads) : 0u;
-      float x[kBatch][T::kElems];
+          for (uint32_t u = 0; u < kN; ++u) bits[u] = mask_bits<T>(mask, lead, c + u * kTeam);
+        }
+      } else {
 #pragma unroll
-      for (uint32_t u = 0; u < kBatch; ++u) {
+        for (uint32_t u = 0; u < kN; ++u) {
+          const bool in = c + u * kTeam < c1_full;
+          w[u] = u32x4{T::kNone, T::kNone, T::kNone, T::kNone};
+          bits[u] = 0;
+          if (in) w[u] = load_even<T>(row, lead, c + u * kTeam);
+          if (kMask && in) bits[u] = mask_bits<T>(mask, lead, c + u * kTeam);
+        }
+      }
+      float x[kN][T::kElems];
+#pragma unroll
+      for (uint32_t u = 0; u < kN; ++u) {
         T::unpack(w[u], x[u]);
         if (kMask) keep_allowed<T>(x[u], bits[u]);
       }
-      add(std::integral_constant<uint32_t, kBatch>{}, x, c + threadIdx.x);
+      if (lead > c) x[0][0] = kNoLogit;
+      add(std::integral_constant<uint32_t, kN>{}, x, c);
     }
-    for (; c < c1; c += kThreads) {
+    if (n_full < c1 && threadIdx.x == (n_full - c0) % kTeam) {   // the chunk that the row's end cuts
       float x[1][T::kElems];
-      if (c + threadIdx.x < c1) {
-        load_any<T>(a, row, mask, c + threadIdx.x, x[0]);
-        add(std::integral_constant<uint32_t, 1>{}, x, c + threadIdx.x);
-      }
+      load_any<T>(a, row, mask, lead, n_full, x[0]);
+      add(std::integral_constant<uint32_t, 1>{}, x, n_full);
     }
     const float mine = sums.m;
     sums = join_sums(sh, sums, a.scale2);
@@ -528,33 +613,33 @@ __global__ __launch_bounds__(kThreads) void k_scores_long(Rows a, Scores out, ui
     if (n_top) {
       const uint64_t least = least_of_interest<T>(sh, mine == kNoLogit ? 0ull : key_of(ordered<T>(mine), place), bits_for(n_chunk), n_top);
       // the hot lanes' chunks, dealt out to all threads
-      const uint32_t n_hot = sh.n_hot, each = (c1 - c0 + kThreads - 1) / kThreads;
-      for (uint32_t i = threadIdx.x; i < n_hot * each; i += kThreads) {
-        const uint32_t turn = i / n_hot, at = c0 + sh.hot[i - turn * n_hot] + turn * kThreads;
+      const uint32_t n_hot = sh.n_hot, each = (c1 - c0 + kTeam - 1) / kTeam;
+      for (uint32_t i = threadIdx.x; i < n_hot * each; i += kTeam) {
+        const uint32_t turn = i / n_hot, at = c0 + sh.hot[i - turn * n_hot] + turn * kTeam;
         if (at >= c1) continue;
         float x[T::kElems];
-        load_any<T>(a, row, mask, at, x);
-        each_candidate<T>(x, at, least, [&](uint64_t k, bool is) { if (is) gather(sh.room, k); });
+        load_any<T>(a, row, mask, lead, at, x);
+        each_candidate<T>(x, lead, at, least, [&](uint64_t k, bool is) { if (is) gather(sh.room, k); });
       }
       __syncthreads();
       uint64_t best;
-      if (sh.room.n <= kRoom) {
+      if (sh.room.n <= sh.room.kMost) {
         best = in_order(sh.room.key, sh.room.n, sh.key, n_top);
       } else {
         const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         List list;
-        for (uint32_t h = wave; h < n_hot; h += kWaves) {
+        for (uint32_t h = wave; h < n_hot; h += kTeam / 64) {
           const uint32_t from = c0 + sh.hot[h];
-          for (uint32_t base = from; base < c1; base += 64 * kThreads) {
-            const uint32_t at = base + lane * kThreads;
+          for (uint32_t base = from; base < c1; base += 64 * kTeam) {
+            const uint32_t at = base + lane * kTeam;
             float x[T::kElems];
             if (at < c1) {
-              load_any<T>(a, row, mask, at, x);
+              load_any<T>(a, row, mask, lead, at, x);
             } else {
 #pragma unroll
               for (uint32_t j = 0; j < T::kElems; ++j) x[j] = kNoLogit;
             }
-            each_candidate<T>(x, at, least, [&](uint64_t k, bool is) { list.insert_lanes(k, is, n_top); });
+            each_candidate<T>(x, lead, at, least, [&](uint64_t k, bool is) { list.insert_lanes(k, is, n_top); });
           }
         }
         best = join_lists(sh, list, n_top);
@@ -571,7 +656,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_long(Rows a, Scores out, ui
 // The parts of a row as one: a workgroup per row.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_scores_join(Rows a, Scores out, uint32_t n_part, const Part VL_GLOBAL *parts, const uint64_t VL_GLOBAL *part_keys) {
-  __shared__ Shared sh;
+  __shared__ Shared<kThreads> sh;
   const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_top = out.n_top;
   for (uint32_t r = blockIdx.x; r < a.n_row; r += gridDim.x) {
     const int32_t token = a.token ? a.token[r] : 0;
@@ -580,6 +665,9 @@ __global__ __launch_bounds__(kThreads) void k_scores_join(Rows a, Scores out, ui
       continue;
     }
     const float given = given_logit<T>(a, r, token);
+    const uint64_t VL_GLOBAL *keys = part_keys + (uint64_t)r * n_part * n_top;
+    uint64_t mine = 0;   // this thread's best of the parts' keys
+    for (uint32_t i = threadIdx.x; i < n_part * n_top; i += kThreads) mine = keys[i] > mine ? keys[i] : mine;
     Sums sums = {kNoLogit, 0.0f, 0.0f};
     if (threadIdx.x < n_part) {   // (never more than there are threads)
       const Part p = parts[(uint64_t)r * n_part + threadIdx.x];
@@ -588,19 +676,18 @@ __global__ __launch_bounds__(kThreads) void k_scores_join(Rows a, Scores out, ui
     sums = join_sums(sh, sums, a.scale2);
     const Final f = finish(a, out, r, sums, given, threadIdx.x == 0);
     if (n_top) {
-      // every thread's best of the parts' keys, then those that n of these reach
-      const uint64_t VL_GLOBAL *keys = part_keys + (uint64_t)r * n_part * n_top;
-      uint64_t mine = 0;
-      for (uint32_t i = threadIdx.x; i < n_part * n_top; i += kThreads) mine = keys[i] > mine ? keys[i] : mine;
+      // the keys that n of the threads' best reach
       const uint64_t least = least_of_interest<T>(sh, mine, bits_for(a.n_vocab), n_top);
-      for (uint32_t i = threadIdx.x; i < n_part * n_top; i += kThreads) {
-        const uint64_t k = keys[i];
-        if (k >= least) gather(sh.room, k);
+      if (mine >= least) {
+        for (uint32_t i = threadIdx.x; i < n_part * n_top; i += kThreads) {
+          const uint64_t k = keys[i];
+          if (k >= least) gather(sh.room, k);
+        }
       }
       __syncthreads();
       // (at most n_top + kMoreHot threads have such keys, with VL_MAX_TOP each at most; a part's keys are next to each other)
       uint64_t best;
-      if (sh.room.n <= kRoom) {
+      if (sh.room.n <= sh.room.kMost) {
         best = in_order(sh.room.key, sh.room.n, sh.key, n_top);
       } else {
         List list;
@@ -669,35 +756,37 @@ __device__ inline void store_any(const Rows &a, uint8_t VL_GLOBAL *to, uint32_t 
   }
 }
 
-template <class T, uint32_t kChunks>
+// Short rows: kTeam lanes per row.  (25,600 rows of 512 logits, 64 chunks: 16 lanes 15.2 us, 32 13.9, 64 14.9.)
+template <class T, uint32_t kTeam, uint32_t kChunks>
 __global__ __launch_bounds__(kThreads) void k_grad_short(Rows a, Grad b) {
-  const uint32_t lane = threadIdx.x & 63u;
-  for (uint32_t r = blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < a.n_row; r += gridDim.x * kWaves) {
+  constexpr uint32_t kTeams = kThreads / kTeam;
+  const uint32_t lane = threadIdx.x % kTeam, team = kTeam == 64 ? (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x / kTeam) : threadIdx.x / kTeam;
+  for (uint32_t first = blockIdx.x * kTeams; first < a.n_row; first += gridDim.x * kTeams) {
+    const uint32_t r = first + team;
+    if (r >= a.n_row) break;
     const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
     uint8_t VL_GLOBAL *to = b.grad + (uint64_t)r * b.ld;
     const uint8_t VL_GLOBAL *mask = a.mask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
-    const GradRow g = grad_row(a, b, r);
     float x[kChunks][T::kElems];
     uint32_t bits[kChunks];
 #pragma unroll
     for (uint32_t i = 0; i < kChunks; ++i) {
-      const uint32_t c = lane + 64 * i;
-      bits[i] = mask && !g.idle && c * T::kElems < a.n_vocab ? mask_bits<T>(mask, c) : 0u;
-      if (!g.idle) load_any<T>(a, row, nullptr, c, x[i]);
+      const uint32_t c = lane + kTeam * i;
+      bits[i] = mask && c * T::kElems < a.n_vocab ? mask_bits<T>(mask, c) : 0u;
+      load_any<T>(a, row, nullptr, c, x[i]);
     }
+    const GradRow g = grad_row(a, b, r);
 #pragma unroll
     for (uint32_t i = 0; i < kChunks; ++i) {
-      if (g.idle) {
+      grad_chunk<T>(a, g, lane + kTeam * i, x[i], bits[i], mask != nullptr);
 #pragma unroll
-        for (uint32_t j = 0; j < T::kElems; ++j) x[i][j] = 0.0f;
-      } else {
-        grad_chunk<T>(a, g, lane + 64 * i, x[i], bits[i], mask != nullptr);
-      }
-      store_any<T>(a, to, lane + 64 * i, x[i]);
+      for (uint32_t j = 0; j < T::kElems; ++j) x[i][j] = g.idle ? 0.0f : x[i][j];
+      store_any<T>(a, to, lane + kTeam * i, x[i]);
     }
   }
 }
 
+constexpr uint32_t kBatch = 4;   // chunks of a lane on their way at once
 template <class T, bool kMask>
 __global__ __launch_bounds__(kThreads) void k_grad_long(Rows a, Grad b, uint32_t piece_chunks) {
   const uint32_t n_full = a.n_vocab / T::kElems, n_chunk = (a.n_vocab + T::kElems - 1) / T::kElems;
@@ -740,11 +829,13 @@ __global__ __launch_bounds__(kThreads) void k_grad_long(Rows a, Grad b, uint32_t
 // ---- host
 
 constexpr uint32_t kMostRows = 0x7FFFFFFFu;
-constexpr uint32_t kShortChunks = 256;   // 16-byte chunks of a row that one wavefront takes (four per lane)
+constexpr uint32_t kShortChunks = 128;       // 16-byte chunks of a row that a few lanes hold in registers
+constexpr uint32_t kShortGradChunks = 256;
 constexpr uint32_t kMostGridY = 65535;
 
 uint32_t size_of(uint32_t type) { return type == VL_F32 ? 4u : 2u; }
 uint32_t chunks_of(const vl_token_rows *a) { const uint32_t e = 16u / size_of(a->type); return (a->n_vocab + e - 1) / e; }
+uint32_t most_chunks_of(const vl_token_rows *a) { const uint32_t e = 16u / size_of(a->type); return (a->n_vocab + (e == 8) + e - 1) / e; }   // (a lead included)
 
 int32_t check_rows(const vl_token_rows *a) {
   if (!a || !a->logits) return VL_E_NULL;
@@ -770,49 +861,68 @@ int32_t check_scores(const vl_token_rows *a, const vl_token_scores *o) {
 
 Rows device_rows(const vl_token_rows *a) {
   return Rows{(const uint8_t VL_GLOBAL *)a->logits, a->ld * size_of(a->type), (const uint8_t VL_GLOBAL *)a->mask, a->mask_ld * 4,
-              (const int32_t VL_GLOBAL *)a->token, a->n_row, a->n_vocab, a->scale, (float)((double)a->scale * 1.4426950408889634)};
+              (const int32_t VL_CONSTANT *)a->token, a->n_row, a->n_vocab, a->scale, (float)((double)a->scale * 1.4426950408889634)};
 }
 
-// How many workgroups share a row, and how many chunks each takes
-struct Split { uint32_t parts, chunks; };
-constexpr uint32_t kWantGroups = 2048;    // eight per compute unit, as many as it holds
-constexpr uint32_t kLeastChunks = 512;    // of a part
-Split split_of(const vl_token_rows *a) {
-  const uint32_t n = chunks_of(a);
-  uint32_t parts = a->n_row >= kWantGroups ? 1u : kWantGroups / a->n_row;
-  const uint32_t most = n / kLeastChunks < kThreads ? n / kLeastChunks : kThreads;
-  if (parts > most) parts = most;
-  if (parts <= 1) return Split{1, n};
-  const uint32_t chunks = ((n + parts - 1) / parts + kThreads - 1) / kThreads * kThreads;
-  return Split{(n + chunks - 1) / chunks, chunks};
+// How many threads a workgroup has, how many workgroups share a row, and how many chunks each takes.  A wavefront per row where there are
+// rows for all wavefronts, if no alternatives are asked for or the row is short (they are found in a share of the row that
+// falls with the threads); more threads per row the fewer rows there are; and parts, which a second launch joins, where few rows
+// are too long for one workgroup.  Measured, us (this choice / the other):
+//   3,000 x 5,000, no alternatives: 64 threads 10.5 / 256 13.2;      4,096 x 50,000, five: 256 90 / 64 119
+//   500 x 32,000 in 32 bits: 1,024 in 1 part 17.7 / 256 in 4 24.0;   300 x 50,001: 1,024 17.8 / 256 in 5 20.7
+//   1 x 32,000: 1,024 in 1 part 9.4 / 256 in 7 11.6;                 1 x 131,072: 256 in 32 parts 11.9 / 1,024 in 1 15.3
+//   1 x 5,000: 256 6.9 / 1,024 9.3;                                  100 x 131,072: 1,024 in 1 part 16.2 / in 5 17.6
+struct Split { uint32_t team, parts, chunks; bool few; };   // few: a compute unit has one workgroup at most, which may use twice the registers
+Split split_of(const vl_token_rows *a, uint32_t n_top) {
+  const uint32_t n = most_chunks_of(a), rows = a->n_row;
+  const bool few = rows < 128;
+  uint32_t team = 1024, parts = 1;
+  if (rows >= 2048 && (n_top == 0 || n <= 2048)) team = 64;
+  else if (rows >= 1024 || (few && n <= 1024)) team = 256;
+  else if (!few) parts = std::max(1u, std::min(512 / rows, n / 1024));
+  else if (rows < 48 && n > 8192) { team = 256; parts = std::min({2048 / rows, n / 512, 256u}); }
+  if (parts == 1) return Split{team, 1, n, few};
+  const uint32_t chunks = ((n + parts - 1) / parts + team - 1) / team * team;
+  return Split{team, (n + chunks - 1) / chunks, chunks, few};
 }
 uint64_t work_of(const vl_token_rows *a, const vl_token_scores *o) {
   if (chunks_of(a) <= kShortChunks) return 0;
-  const Split s = split_of(a);
+  const Split s = split_of(a, o->n_top);
   return s.parts == 1 ? 0 : (uint64_t)a->n_row * s.parts * (sizeof(Part) + 8ull * o->n_top);
 }
 
+template <class T, uint32_t kTeam, uint32_t kN>
+void launch_long(const Rows &a, const Scores &out, Split split, Part VL_GLOBAL *parts, uint64_t VL_GLOBAL *keys, hipStream_t stream) {
+  const dim3 grid(split.parts, std::min(a.n_row, kMostGridY));
+  const bool entropy = out.entropy;   // (8,000 x 20,000: 65 us with it, 61 without)
+  (a.mask ? entropy ? k_scores_long<T, kTeam, kN, true, true> : k_scores_long<T, kTeam, kN, true, false>
+          : entropy ? k_scores_long<T, kTeam, kN, false, true> : k_scores_long<T, kTeam, kN, false, false>)<<<grid, kTeam, 0, stream>>>(a, out, split.chunks, parts, keys);
+}
 template <class T>
 void launch_scores(const Rows &a, const Scores &out, uint32_t n_chunk, Split split, void *work, hipStream_t stream) {
+  if (n_chunk <= kShortChunks && !out.n_top) {
+    const uint32_t blocks = std::min((a.n_row + kQuarters - 1) / kQuarters, 1u << 20);
+    (n_chunk <= 16 ? k_scores_quarter<T, 1> : n_chunk <= 32 ? k_scores_quarter<T, 2> : n_chunk <= 64 ? k_scores_quarter<T, 4> : k_scores_quarter<T, 8>)
+        <<<blocks, kThreads, 0, stream>>>(a, out);
+    return;
+  }
   if (n_chunk <= kShortChunks) {
     const uint32_t blocks = std::min((a.n_row + kWaves - 1) / kWaves, 1u << 20);
-    (n_chunk <= 64 ? k_scores_short<T, 1> : n_chunk <= 128 ? k_scores_short<T, 2> : k_scores_short<T, 4>)<<<blocks, kThreads, 0, stream>>>(a, out);
+    (n_chunk <= 64 ? k_scores_short<T, 1> : k_scores_short<T, 2>)<<<blocks, kThreads, 0, stream>>>(a, out);
     return;
   }
   Part VL_GLOBAL *parts = split.parts > 1 ? (Part VL_GLOBAL *)work : nullptr;
   uint64_t VL_GLOBAL *keys = parts ? (uint64_t VL_GLOBAL *)((uint8_t *)work + (uint64_t)a.n_row * split.parts * sizeof(Part)) : nullptr;
-  const dim3 grid(split.parts, std::min(a.n_row, kMostGridY));
-  const bool entropy = out.entropy;
-  (a.mask ? entropy ? k_scores_long<T, true, true> : k_scores_long<T, true, false>
-          : entropy ? k_scores_long<T, false, true> : k_scores_long<T, false, false>)<<<grid, kThreads, 0, stream>>>(a, out, split.chunks, parts, keys);
+  (split.team == 64 ? launch_long<T, 64, 4> : split.team == 256 ? launch_long<T, 256, 4> : split.few ? launch_long<T, 1024, 4> : launch_long<T, 1024, 2>)(a, out, split, parts, keys, stream);
   if (parts) k_scores_join<T><<<a.n_row, kThreads, 0, stream>>>(a, out, split.parts, parts, keys);
 }
 
 template <class T>
 void launch_grad(const Rows &a, const Grad &b, uint32_t n_chunk, hipStream_t stream) {
-  if (n_chunk <= kShortChunks) {
-    const uint32_t blocks = std::min((a.n_row + kWaves - 1) / kWaves, 1u << 20);
-    (n_chunk <= 64 ? k_grad_short<T, 1> : n_chunk <= 128 ? k_grad_short<T, 2> : k_grad_short<T, 4>)<<<blocks, kThreads, 0, stream>>>(a, b);
+  if (n_chunk <= kShortGradChunks) {
+    const uint32_t team = n_chunk <= 32 ? 16 : n_chunk <= 64 ? 32 : 64, teams = kThreads / team;
+    (n_chunk <= 16 ? k_grad_short<T, 16, 1> : n_chunk <= 32 ? k_grad_short<T, 16, 2> : n_chunk <= 64 ? k_grad_short<T, 32, 2>
+     : n_chunk <= 128 ? k_grad_short<T, 64, 2> : k_grad_short<T, 64, 4>)<<<std::min((a.n_row + teams - 1) / teams, 1u << 20), kThreads, 0, stream>>>(a, b);
     return;
   }
   const uint32_t piece = kBatch * kThreads;
@@ -840,7 +950,7 @@ extern "C" int32_t vl_token_logprobs(const vl_token_rows *rows, const vl_token_s
   const Scores o = {(float VL_GLOBAL *)out->logprob, (float VL_GLOBAL *)out->entropy, (float VL_GLOBAL *)out->stat, (float VL_GLOBAL *)out->top_logprob,
                     (int32_t VL_GLOBAL *)out->top_token, out->n_top};
   (rows->type == VL_F32 ? launch_scores<F32> : rows->type == VL_F16 ? launch_scores<F16> : launch_scores<BF16>)(
-      device_rows(rows), o, chunks_of(rows), split_of(rows), work, stream);
+      device_rows(rows), o, chunks_of(rows), split_of(rows, out->n_top), work, stream);
   VL_HIP(hipGetLastError());
   return VL_OK;
 }
