@@ -9,7 +9,7 @@ BENCH_SOURCES = ["vl_probe.hip"]   # measurement hooks of the benchmark (include
 LIB = os.path.join(HERE, "libvl.so")
 BENCH_LIB = os.path.join(HERE, "libvlbench.so")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall",
-         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-parallel-jobs=8"]
 
 
 def stale() -> bool:

@@ -122,6 +122,11 @@ __device__ inline u32x4 load_even(const uint8_t VL_GLOBAL *row, uint32_t lead, u
   typedef u32x4 words __attribute__((aligned(4)));
   return *(const words VL_GLOBAL *)(row - lead * 2 + (uint64_t)c * 16);
 }
+template <class T>
+__device__ inline u32x4 load_once(const uint8_t VL_GLOBAL *row, uint32_t lead, uint32_t c) {   // nothing of it is kept in the caches
+  typedef u32x4 words __attribute__((aligned(4)));
+  return __builtin_nontemporal_load((const words VL_GLOBAL *)(row - lead * 2 + (uint64_t)c * 16));
+}
 
 // the logits that the mask does not allow become -infinity (bit j of `bits`: logit j is allowed)
 template <class T>
@@ -158,7 +163,43 @@ __device__ inline void load_any(const Rows &a, const uint8_t VL_GLOBAL *row, con
   if (mask) keep_allowed<T>(x, from < a.n_vocab ? mask_bits<T>(mask, c) : 0u);
 }
 
-// the same with `lead`
+// Chunks lane, lane + kStride, ... of a short row, into bits what the mask says of them (all ones without one).  All loads are on their way
+// before the first is waited for.
+template <class T, uint32_t kStride, uint32_t kChunks>
+__device__ inline void load_row(const Rows &a, const uint8_t VL_GLOBAL *row, const uint8_t VL_GLOBAL *mask, uint32_t lane, float (*x)[T::kElems], uint32_t *bits) {
+  u32x4 w[kChunks];
+#pragma unroll
+  for (uint32_t i = 0; i < kChunks; ++i) {
+    const uint32_t c = lane + kStride * i;
+    w[i] = u32x4{T::kNone, T::kNone, T::kNone, T::kNone};
+    if ((c + 1) * T::kElems <= a.n_vocab) w[i] = load_chunk<T>(row, c);
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < kChunks; ++i) {
+    const uint32_t c = lane + kStride * i;
+    bits[i] = ~0u;
+    if (mask && c * T::kElems < a.n_vocab) bits[i] = mask_bits<T>(mask, c);
+  }
+  const uint32_t cut = a.n_vocab / T::kElems;   // the chunk that the row's end cuts, if it does
+  float last[T::kElems];
+  if (a.n_vocab % T::kElems) {
+#pragma unroll
+    for (uint32_t j = 0; j < T::kElems; ++j) {
+      const uint32_t t = cut * T::kElems + j;
+      last[j] = t < a.n_vocab ? T::wide(((const typename T::type VL_GLOBAL *)row)[t]) : kNoLogit;
+    }
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < kChunks; ++i) T::unpack(w[i], x[i]);
+  if (a.n_vocab % T::kElems) {
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i)
+#pragma unroll
+      for (uint32_t j = 0; j < T::kElems; ++j) x[i][j] = lane + kStride * i == cut ? last[j] : x[i][j];
+  }
+}
+
+// a chunk of a long row, with its lead
 template <class T>
 __device__ inline void load_any(const Rows &a, const uint8_t VL_GLOBAL *row, const uint8_t VL_GLOBAL *mask, uint32_t lead, uint32_t c, float *x) {
   const uint32_t from = c * T::kElems - lead;   // (2^32 - 1 in front of the row)
@@ -355,9 +396,12 @@ __global__ __launch_bounds__(kThreads) void k_scores_quarter(Rows a, Scores out)
     const uint8_t VL_GLOBAL *mask = a.mask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
     const int32_t token = a.token ? a.token[r] : 0;
     float x[kChunks][T::kElems];
-#pragma unroll
-    for (uint32_t i = 0; i < kChunks; ++i) load_any<T>(a, row, mask, lane + 16 * i, x[i]);
+    uint32_t bits[kChunks];
+    load_row<T, 16, kChunks>(a, row, mask, lane, x, bits);
     const float given = given_logit<T>(a, r, token);
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i)
+      if (mask) keep_allowed<T>(x[i], bits[i]);
     float m = kNoLogit;
 #pragma unroll
     for (uint32_t i = 0; i < kChunks; ++i)
@@ -395,9 +439,12 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
       continue;
     }
     float x[kChunks][T::kElems];
-#pragma unroll
-    for (uint32_t i = 0; i < kChunks; ++i) load_any<T>(a, row, mask, lane + 64 * i, x[i]);
+    uint32_t bits[kChunks];
+    load_row<T, 64, kChunks>(a, row, mask, lane, x, bits);
     const float given = given_logit<T>(a, r, token);
+#pragma unroll
+    for (uint32_t i = 0; i < kChunks; ++i)
+      if (mask) keep_allowed<T>(x[i], bits[i]);
     float m = kNoLogit;
     uint32_t place = 0;
 #pragma unroll
@@ -524,12 +571,15 @@ __device__ inline Sums join_sums(Shared<kTeam> &sh, Sums mine, float scale2) {
 }
 
 
+// what is asked for: alternatives too, sums alone, or sums alone of logits of which nothing is kept in the caches
+enum Kind { kWithTop, kSums, kSumsOnce };
+
 // Long rows: a workgroup of kTeam threads per row or part of a row.  Thread t takes the part's chunks t, t + kTeam, t + 2 kTeam, ...
 // kN chunks of a lane are on their way at once.
-template <class T, uint32_t kTeam, uint32_t kN, bool kMask, bool kEntropy>
+template <class T, uint32_t kTeam, uint32_t kN, bool kMask, Kind kKind>
 __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_scores_long(Rows a, Scores out, uint32_t part_chunks, Part VL_GLOBAL *parts, uint64_t VL_GLOBAL *part_keys) {
   __shared__ Shared<kTeam> sh;
-  const uint32_t c0 = blockIdx.x * part_chunks, n_top = out.n_top;
+  const uint32_t c0 = blockIdx.x * part_chunks, n_top = kKind == kWithTop ? out.n_top : 0;
   for (uint32_t r = blockIdx.y; r < a.n_row; r += gridDim.y) {
     const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
     const uint8_t VL_GLOBAL *mask = kMask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
@@ -568,7 +618,7 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
         for (uint32_t j = 0; j < T::kElems; ++j) {
           const float z = (x[u][j] - ref) * a.scale2, e = __builtin_amdgcn_exp2f(z);
           sums.s += e;
-          if (kEntropy) sums.y += e * fmaxf(z, kFar);
+          sums.y += e * fmaxf(z, kFar);
         }
     };
     for (uint32_t c = c0 + threadIdx.x; c - threadIdx.x < c1_full; c += kN * kTeam) {
@@ -576,7 +626,7 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
       uint32_t bits[kN];
       if (c - threadIdx.x + kN * kTeam <= c1_full) {
 #pragma unroll
-        for (uint32_t u = 0; u < kN; ++u) w[u] = load_even<T>(row, lead, c + u * kTeam);
+        for (uint32_t u = 0; u < kN; ++u) w[u] = kKind == kSumsOnce ? load_once<T>(row, lead, c + u * kTeam) : load_even<T>(row, lead, c + u * kTeam);
         if (kMask) {
 #pragma unroll
           for (uint32_t u = 0; u < kN; ++u) bits[u] = mask_bits<T>(mask, lead, c + u * kTeam);
@@ -744,11 +794,12 @@ __device__ inline void grad_chunk(const Rows &a, const GradRow &g, uint32_t c, f
       x[j] = as_float(as_word(x[j]) & (uint32_t)((int32_t)(bits << (31 - j)) >> 31));
   }
 }
+// (not kept in the caches of a die, which others could not use: 25,600 rows of 1,024 25.8 -> 22.4 us)
 template <class T>
 __device__ inline void store_any(const Rows &a, uint8_t VL_GLOBAL *to, uint32_t c, const float *x) {
   const uint32_t from = c * T::kElems;
   if (from + T::kElems <= a.n_vocab) {
-    *(typename T::chunk VL_GLOBAL *)(to + (uint64_t)c * 16) = T::pack(x);
+    __builtin_nontemporal_store(T::pack(x), (typename T::chunk VL_GLOBAL *)(to + (uint64_t)c * 16));
   } else {
 #pragma unroll
     for (uint32_t j = 0; j < T::kElems; ++j)
@@ -756,7 +807,8 @@ __device__ inline void store_any(const Rows &a, uint8_t VL_GLOBAL *to, uint32_t 
   }
 }
 
-// Short rows: kTeam lanes per row.  (25,600 rows of 512 logits, 64 chunks: 16 lanes 15.2 us, 32 13.9, 64 14.9.)
+// Short rows: kTeam lanes per row, eight workgroups per compute unit.  (25,600 rows of 512 logits, 64 chunks: 16 and 32 lanes 12.7 us, 64
+// 14.5; as many workgroups as it takes 13.3.)
 template <class T, uint32_t kTeam, uint32_t kChunks>
 __global__ __launch_bounds__(kThreads) void k_grad_short(Rows a, Grad b) {
   constexpr uint32_t kTeams = kThreads / kTeam;
@@ -769,12 +821,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_short(Rows a, Grad b) {
     const uint8_t VL_GLOBAL *mask = a.mask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
     float x[kChunks][T::kElems];
     uint32_t bits[kChunks];
-#pragma unroll
-    for (uint32_t i = 0; i < kChunks; ++i) {
-      const uint32_t c = lane + kTeam * i;
-      bits[i] = mask && c * T::kElems < a.n_vocab ? mask_bits<T>(mask, c) : 0u;
-      load_any<T>(a, row, nullptr, c, x[i]);
-    }
+    load_row<T, kTeam, kChunks>(a, row, mask, lane, x, bits);
     const GradRow g = grad_row(a, b, r);
 #pragma unroll
     for (uint32_t i = 0; i < kChunks; ++i) {
@@ -894,9 +941,13 @@ uint64_t work_of(const vl_token_rows *a, const vl_token_scores *o) {
 template <class T, uint32_t kTeam, uint32_t kN>
 void launch_long(const Rows &a, const Scores &out, Split split, Part VL_GLOBAL *parts, uint64_t VL_GLOBAL *keys, hipStream_t stream) {
   const dim3 grid(split.parts, std::min(a.n_row, kMostGridY));
-  const bool entropy = out.entropy;   // (8,000 x 20,000: 65 us with it, 61 without)
-  (a.mask ? entropy ? k_scores_long<T, kTeam, kN, true, true> : k_scores_long<T, kTeam, kN, true, false>
-          : entropy ? k_scores_long<T, kTeam, kN, false, true> : k_scores_long<T, kTeam, kN, false, false>)<<<grid, kTeam, 0, stream>>>(a, out, split.chunks, parts, keys);
+  // Logits beyond what the Infinity Cache holds (256 MB) are not kept in the caches: 1,500 rows of 131,072 77 -> 69 us,
+  // 8,000 of 20,000 65 -> 56; but 64 MB that the program before has just written 17.7 -> 19.9.  With alternatives, whose chunks are read
+  // again, it makes no difference (4,096 x 50,001 and five of them: 89).
+  const bool once = (uint64_t)a.n_row * a.n_vocab * sizeof(typename T::type) > (256ull << 20);
+  (a.mask ? out.n_top ? k_scores_long<T, kTeam, kN, true, kWithTop> : once ? k_scores_long<T, kTeam, kN, true, kSumsOnce> : k_scores_long<T, kTeam, kN, true, kSums>
+          : out.n_top ? k_scores_long<T, kTeam, kN, false, kWithTop> : once ? k_scores_long<T, kTeam, kN, false, kSumsOnce> : k_scores_long<T, kTeam, kN, false, kSums>)
+      <<<grid, kTeam, 0, stream>>>(a, out, split.chunks, parts, keys);
 }
 template <class T>
 void launch_scores(const Rows &a, const Scores &out, uint32_t n_chunk, Split split, void *work, hipStream_t stream) {
@@ -922,7 +973,7 @@ void launch_grad(const Rows &a, const Grad &b, uint32_t n_chunk, hipStream_t str
   if (n_chunk <= kShortGradChunks) {
     const uint32_t team = n_chunk <= 32 ? 16 : n_chunk <= 64 ? 32 : 64, teams = kThreads / team;
     (n_chunk <= 16 ? k_grad_short<T, 16, 1> : n_chunk <= 32 ? k_grad_short<T, 16, 2> : n_chunk <= 64 ? k_grad_short<T, 32, 2>
-     : n_chunk <= 128 ? k_grad_short<T, 64, 2> : k_grad_short<T, 64, 4>)<<<std::min((a.n_row + teams - 1) / teams, 1u << 20), kThreads, 0, stream>>>(a, b);
+     : n_chunk <= 128 ? k_grad_short<T, 64, 2> : k_grad_short<T, 64, 4>)<<<std::min((a.n_row + teams - 1) / teams, 2048u), kThreads, 0, stream>>>(a, b);
     return;
   }
   const uint32_t piece = kBatch * kThreads;
