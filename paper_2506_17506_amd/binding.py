@@ -380,10 +380,17 @@ VL_F32, VL_F16, VL_BF16 = 0, 1, 2
 VL_MAX_VOCAB, VL_MAX_TOP = 1 << 24, 32
 POLICY_STATS_DTYPE = np.dtype([("loss", "<f4"), ("kl", "<f4"), ("n_token", "<u8"), ("n_clipped", "<u8")])   # vl_policy_stats
 # the structures' fields as bytes, which is quicker than a ctypes structure per call
-_PACK_ROWS = struct.Struct("<QQQQQIIIf").pack
-_PACK_SCORES = struct.Struct("<QQQQQII").pack
-_PACK_WEIGHTS = struct.Struct("<ffff").pack
-_PACK_BATCH = struct.Struct("<QQQQQQQQIIfffI").pack
+_ROWS, _SCORES = struct.Struct("<QQQQQIIIf").pack, struct.Struct("<QQQQQII").pack
+_WEIGHTS, _BATCH = struct.Struct("<ffff").pack, struct.Struct("<QQQQQQQQIIfffI").pack
+_ELSEWHERE = " (a tensor is not on the current device)"
+
+
+def _packed(what, pack, *fields):
+    try:
+        return pack(*fields)
+    except (struct.error, OverflowError):   # a size or a number that its field does not hold
+        raise VlError(-3, what) from None
+
 
 
 class _Torch:
@@ -415,7 +422,7 @@ def _device_of(x, what):
         _t = _Torch()
     if x.is_cuda and x.get_device() == _t.device():
         return x.get_device()
-    raise VlError(-7, what)
+    raise VlError(-7, what + _ELSEWHERE)
 
 
 def _tensor(what, x, dtypes, shape, device, nullable=True):
@@ -425,7 +432,7 @@ def _tensor(what, x, dtypes, shape, device, nullable=True):
             return 0
         raise VlError(-1, what)
     if x.get_device() != device:
-        raise VlError(-7, what)
+        raise VlError(-7, what + _ELSEWHERE)
     if x.dtype not in dtypes:
         raise VlError(-3, what)
     if (shape is not None and x.shape != shape) or not x.is_contiguous():
@@ -453,7 +460,7 @@ def _token_rows(what, logits, token, mask, scale):
     p_mask = mask_ld = 0
     if mask is not None:
         if mask.get_device() != device:
-            raise VlError(-7, what)
+            raise VlError(-7, what + _ELSEWHERE)
         if mask.dtype not in _t.words:
             raise VlError(-3, what)
         shared = mask.dim() == 1
@@ -461,7 +468,7 @@ def _token_rows(what, logits, token, mask, scale):
             raise VlError(-2, what)
         p_mask, mask_ld = mask.data_ptr(), 0 if shared or n == 1 else mask.stride(0)
     p_token = 0 if token is None else _tensor(what, token, _t.words[:1], (n,), device)
-    return _PACK_ROWS(logits.data_ptr(), ld, p_mask, mask_ld, p_token, n, v, kind, scale), n, v, device
+    return _packed(what, _ROWS, logits.data_ptr(), ld, p_mask, mask_ld, p_token, n, v, kind, scale), n, v, device
 
 
 def _call_stream(stream, device):
@@ -480,7 +487,7 @@ def _work(what, n_bytes, work, stream, device):
     """(pointer, bytes, the tensor): `work`, or n_bytes of the call's own, allocated on the stream it runs on"""
     if work is not None:
         if work.get_device() != device:
-            raise VlError(-7, what)
+            raise VlError(-7, what + _ELSEWHERE)
         if not work.is_contiguous():
             raise VlError(-2, what)
     elif not n_bytes:
@@ -503,7 +510,7 @@ def _token_scores(logits, token, mask, scale, logprob, entropy, stat, top_token,
         if some.dim() != 2:
             raise VlError(-2, what)
         k = some.shape[1]
-    return rows, _PACK_SCORES(_tensor(what, logprob, f, (n,), device), _tensor(what, entropy, f, (n,), device), _tensor(what, stat, f, (n, 2), device),
+    return rows, _packed(what, _SCORES, _tensor(what, logprob, f, (n,), device), _tensor(what, entropy, f, (n,), device), _tensor(what, stat, f, (n, 2), device),
                               _tensor(what, top_token, _t.words[:1], (n, k), device), _tensor(what, top_logprob, f, (n, k), device), k, 0), device
 
 
@@ -537,7 +544,7 @@ def vl_token_logprobs_grad(logits, stat, grad, token=None, mask=None, scale=1.0,
     if grad is None:
         raise VlError(-1, what)
     if grad.get_device() != device:
-        raise VlError(-7, what)
+        raise VlError(-7, what + _ELSEWHERE)
     if grad.dtype != logits.dtype:
         raise VlError(-3, what)
     if grad.shape != logits.shape:
@@ -559,11 +566,11 @@ def vl_group_advantages(counts, group_off, weights, eps, advantage, reward=None,
     if some is None:
         raise VlError(-1, what)
     shape, n, f = some.shape, some.numel(), _t.f32
-    p = _tensor(what, counts, _t.record, None, device)
+    p = _tensor(what, counts, _t.record[:3], None, device)
     if counts is not None and counts.numel() * counts.element_size() != 32 * n:
         raise VlError(-2, what)
     rc = _lib.vl_group_advantages(p, _tensor(what, extra, f, shape, device), n, _tensor(what, group_off, _t.words, None, device),
-                                  max(0, group_off.numel() - 1), _PACK_WEIGHTS(*weights), eps, _tensor(what, reward, f, shape, device),
+                                  max(0, group_off.numel() - 1), _packed(what, _WEIGHTS, *weights), eps, _tensor(what, reward, f, shape, device),
                                   _tensor(what, advantage, f, shape, device), _call_stream(stream, device))
     if rc != 0:
         raise VlError(rc, what)
@@ -579,7 +586,7 @@ def _policy_batch(logprob, logprob_old, start, length, advantage, weight, log_lo
     m = start.numel()
     if max_len is None:   # the mean length, if there is no room between the samples: a launch's shape, not a bound
         max_len = min(0xFFFFFFFF, n // max(1, m) + 1)
-    return _PACK_BATCH(_tensor(what, logprob, f, None, device), _tensor(what, logprob_old, f, shape, device, False),
+    return _packed(what, _BATCH, _tensor(what, logprob, f, None, device), _tensor(what, logprob_old, f, shape, device, False),
                        _tensor(what, logprob_ref, f, shape, device), n, _tensor(what, start, _t.longs, None, device),
                        _tensor(what, length, _t.words, samples, device, False), _tensor(what, advantage, f, samples, device, False),
                        _tensor(what, weight, f, samples, device, False), m, max_len, log_lo, log_hi, kl, 0), device

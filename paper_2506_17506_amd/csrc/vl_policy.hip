@@ -119,11 +119,11 @@ constexpr uint32_t kGroups = 2, kStep = kGroups * 256;   // a lane takes kGroups
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 
-// exp(q) - q - 1 and exp(q) - 1.  Near 0 from the series of the first, q^2 (1/2 + q/6 + ... + q^6/40320), whose next term is
-// below 2^-30 of the sum for |q| < 1/4: the difference would cancel.
+// exp(q) - q - 1 and exp(q) - 1.  Near 0 from the series of the first, q^2 (1/2 + q/6 + ... + q^7/362880), whose next term is
+// below 2^-28 of the sum for |q| < 1/2: the difference would cancel.
 __device__ inline void exp_gap(float q, float &gap, float &less_one) {
-  if (fabsf(q) < 0.25f) {
-    gap = q * q * (0.5f + q * (1.0f / 6 + q * (1.0f / 24 + q * (1.0f / 120 + q * (1.0f / 720 + q * (1.0f / 5040 + q * (1.0f / 40320)))))));
+  if (fabsf(q) < 0.5f) {
+    gap = q * q * (0.5f + q * (1.0f / 6 + q * (1.0f / 24 + q * (1.0f / 120 + q * (1.0f / 720 + q * (1.0f / 5040 + q * (1.0f / 40320 + q * (1.0f / 362880))))))));
     less_one = gap + q;
   } else {
     const float e = expf(q);

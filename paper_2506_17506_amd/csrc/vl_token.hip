@@ -301,7 +301,7 @@ __device__ inline uint32_t bits_for(uint32_t n) { return 32u - (uint32_t)__built
 
 // Where keys that may be among a row's n best are gathered.  More than there is room for are possible (many equal
 // logits, or a row sorted in an unlucky way); then the row's best are found by insertion instead.
-constexpr uint32_t kMoreHot = 8;   // more than n lanes may have their chunks looked at again, so that the search for them ends sooner
+constexpr uint32_t kMoreHot = 4;   // more than n lanes may have their chunks looked at again, so that the search for them ends sooner
 template <uint32_t kTeam>
 struct Room {
   static constexpr uint32_t kMost = kTeam < 256 ? kTeam : 256;   // (one per thread is put in order)

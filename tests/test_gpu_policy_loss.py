@@ -250,3 +250,26 @@ def test_equal_calls_give_equal_bits():
         call(d, grad, stats)
         got.append((grad.cpu(), stats.cpu()))
     assert all((g == got[0][0]).all() and (s == got[0][1]).all() for g, s in got)
+
+
+def test_refusals_of_the_binding():
+    d = device(make([0], [40], 40, 6))
+    grad, stats = torch.zeros(40, device="cuda"), torch.zeros(24, dtype=torch.uint8, device="cuda")
+
+    def code(g=grad, st=stats, lo=-0.25, kl=0.1, **change):
+        with pytest.raises(vl.VlError) as err:
+            call({**d, **change}, g, st, lo=lo, kl=kl)
+        return err.value.code
+    assert code(g=grad[:39]) == -2 and code(g=grad.half()) == -3 and code(g=None) == -1 and code(g=grad.cpu()) == -7
+    assert code(st=stats[:20]) == -2 and code(old=d["old"].cpu()) == -7 and code(old=d["old"][::2]) == -2 and code(lp=None) == -1
+    assert code(start=d["start"].int()) == -3 and code(length=d["length"].long()) == -3 and code(adv=None) == -1
+    assert code(weight=d["weight"].double()) == -3 and code(lo=0.5) == -3 and code(ref=None) == -1 and code(kl=float("nan")) == -3
+    c, adv = torch.from_numpy(some_counts(8, 1)).cuda(), torch.zeros(8, device="cuda")
+    off = torch.tensor([0, 8], dtype=torch.int32, device="cuda")
+    for args, want in (((c[:7], off, W, 1e-6, adv), -2), ((c.long(), off, W, 1e-6, adv), -3), ((c, off.cpu(), W, 1e-6, adv), -7), ((c, off[:1], W, 1e-6, adv), -2),
+                       ((c, off, W, 0.0, adv), -3), ((c, off, (1e300, 0, 0, 0), 1e-6, adv), -3), ((None, off, W, 1e-6, adv), -1), ((c, off, W, 1e-6, None), -1)):
+        with pytest.raises(vl.VlError) as err:
+            vl.vl_group_advantages(*args)
+        assert err.value.code == want, args
+    torch.cuda.synchronize()
+    assert (grad == 0).all() and (adv == 0).all()

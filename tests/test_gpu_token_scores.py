@@ -354,6 +354,55 @@ def test_two_streams_and_a_recorded_pass():
         near(grad, d, err, "replayed gradient")
 
 
+@pytest.mark.parametrize("n,v,top", [(1, 131072, 20), (300, 20011, 5), (3000, 512, 8), (2500, 4097, 0), (700, 300, 0)])
+def test_equal_calls_give_equal_bits(n, v, top):
+    x, t = bell(n, v, BF16, 1), tokens(n, v, 2)
+    first = scores(x, t, top=top)
+    g = torch.randn(n, generator=torch.Generator().manual_seed(3)).cuda()
+    grads = []
+    for _ in range(4):
+        again = scores(x, t, top=top)
+        for name in first:
+            assert torch.equal(first[name], again[name]), name
+        grads.append(torch.empty_like(x))
+        vl.vl_token_logprobs_grad(x, again["stat"], grads[-1], token=t, entropy=again["entropy"], g_logprob=g, g_entropy=g)
+    assert all(torch.equal(grads[0], y) for y in grads)
+
+
+def test_refusals_of_the_binding():
+    x = torch.zeros((4, 64), device="cuda")
+    out = torch.zeros(4, device="cuda")
+    t = torch.zeros(4, dtype=torch.int32, device="cuda")
+
+    def code(*args, **named):
+        with pytest.raises(vl.VlError) as err:
+            vl.vl_token_logprobs(*args, **named)
+        return err.value.code
+    assert code(x, entropy=out.cpu()) == -7
+    assert code(x, token=t.cpu(), logprob=out) == -7
+    assert code(x, mask=torch.zeros((4, 2), dtype=torch.int32), entropy=out) == -7
+    assert code(x.double(), entropy=out) == -3
+    assert code(x, entropy=out.half()) == -3
+    assert code(x, token=t.long(), logprob=out) == -3
+    assert code(x.t(), entropy=out) == -2                        # rows that are not contiguous
+    assert code(x[0], entropy=out) == -2
+    assert code(x, entropy=out[:3]) == -2
+    assert code(x, entropy=torch.zeros(8, device="cuda")[::2]) == -2
+    assert code(x, mask=torch.zeros((4, 1), dtype=torch.int32, device="cuda"), entropy=out) == -2
+    assert code(x[:1].expand(4, 64), entropy=out) == -2          # rows of no pitch
+    assert code(x, token=t) == -1 and code(x, logprob=out) == -1
+    assert code(x, entropy=out, scale=0.0) == -3 and code(x, entropy=out, scale=1e300) == -3
+    assert code(x[:0], entropy=out[:0]) == -2 and code(x[:, :0], entropy=out) == -3
+    assert code(x, top_token=torch.zeros((4, 33), dtype=torch.int32, device="cuda")) == -3
+    stat = torch.zeros((4, 2), device="cuda")
+    for grad, want in ((torch.zeros((4, 63), device="cuda"), -2), (x.half(), -3), (x.cpu(), -7), (None, -1)):
+        with pytest.raises(vl.VlError) as err:
+            vl.vl_token_logprobs_grad(x, stat, grad, token=t, g_logprob=out)
+        assert err.value.code == want
+    torch.cuda.synchronize()
+    assert (out == 0).all()
+
+
 def test_work_of_the_callers():
     x, t = bell(1, 131072, BF16, 1), tokens(1, 131072, 1)
     lp = torch.zeros(1, device="cuda")
