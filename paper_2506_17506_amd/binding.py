@@ -457,6 +457,8 @@ def _token_rows(what, logits, token, mask, scale):
         raise VlError(-3, what)
     ld = _row_pitch(what, logits)
     n, v = logits.shape
+    if not n or not v:   # (an empty tensor has no pointer)
+        raise VlError(-3 if n else -2, what)
     p_mask = mask_ld = 0
     if mask is not None:
         if mask.get_device() != device:
@@ -566,6 +568,8 @@ def vl_group_advantages(counts, group_off, weights, eps, advantage, reward=None,
     if some is None:
         raise VlError(-1, what)
     shape, n, f = some.shape, some.numel(), _t.f32
+    if not n:
+        raise VlError(-2, what)
     p = _tensor(what, counts, _t.record[:3], None, device)
     if counts is not None and counts.numel() * counts.element_size() != 32 * n:
         raise VlError(-2, what)
@@ -584,6 +588,8 @@ def _policy_batch(logprob, logprob_old, start, length, advantage, weight, log_lo
         raise VlError(-1, what)
     f, shape, samples, n = _t.f32, logprob.shape, start.shape, logprob.numel()
     m = start.numel()
+    if not n or not m:
+        raise VlError(-2, what)
     if max_len is None:   # the mean length, if there is no room between the samples: a launch's shape, not a bound
         max_len = min(0xFFFFFFFF, n // max(1, m) + 1)
     return _packed(what, _BATCH, _tensor(what, logprob, f, None, device), _tensor(what, logprob_old, f, shape, device, False),

@@ -264,10 +264,11 @@ def test_refusals_of_the_binding():
     assert code(st=stats[:20]) == -2 and code(old=d["old"].cpu()) == -7 and code(old=d["old"][::2]) == -2 and code(lp=None) == -1
     assert code(start=d["start"].int()) == -3 and code(length=d["length"].long()) == -3 and code(adv=None) == -1
     assert code(weight=d["weight"].double()) == -3 and code(lo=0.5) == -3 and code(ref=None) == -1 and code(kl=float("nan")) == -3
+    assert code(start=d["start"][:0], length=d["length"][:0], adv=d["adv"][:0], weight=d["weight"][:0]) == -2
     c, adv = torch.from_numpy(some_counts(8, 1)).cuda(), torch.zeros(8, device="cuda")
     off = torch.tensor([0, 8], dtype=torch.int32, device="cuda")
     for args, want in (((c[:7], off, W, 1e-6, adv), -2), ((c.long(), off, W, 1e-6, adv), -3), ((c, off.cpu(), W, 1e-6, adv), -7), ((c, off[:1], W, 1e-6, adv), -2),
-                       ((c, off, W, 0.0, adv), -3), ((c, off, (1e300, 0, 0, 0), 1e-6, adv), -3), ((None, off, W, 1e-6, adv), -1), ((c, off, W, 1e-6, None), -1)):
+                       ((c, off, W, 0.0, adv), -3), ((c, off, (1e300, 0, 0, 0), 1e-6, adv), -3), ((None, off, W, 1e-6, adv), -1), ((c, off, W, 1e-6, None), -1), ((c[:0], off, W, 1e-6, adv[:0]), -2)):
         with pytest.raises(vl.VlError) as err:
             vl.vl_group_advantages(*args)
         assert err.value.code == want, args
