@@ -10,8 +10,8 @@
 //
 // The n best of a row cost the loop next to nothing: a lane also keeps which of its chunks its m came from.  The n lanes
 // with the best (m, chunk) hold all of the row's n best: any other lane's best is below n
-// larger ones.  Their chunks, n / 256 of the row, are read again, and what is not below the worst of those n maxima, seldom more
-// than n logits, is put in order by counting, for each, how many are better.
+// larger ones.  Those chunks are read again, and all chunks of such a lane if its second best chunk reaches the worst of those n
+// maxima too; what does, seldom much more than n logits, is put in order by counting, for each, how many are better.
 #include <algorithm>
 #include <type_traits>
 
@@ -533,7 +533,7 @@ __device__ inline uint64_t join_lists(Shared<kTeam> &sh, const List &list, uint3
   __syncthreads();
   return in_order(sh.list, kTeam / 64 * n, sh.key, n);
 }
-// A key that n of the threads' best, `mine`, reach, and not many more; the threads whose best reaches it are listed as hot
+// A key that n of the threads' best, `mine`, reach, and not many more
 template <class T, uint32_t kTeam>
 __device__ inline uint64_t least_of_interest(Shared<kTeam> &sh, uint64_t mine, uint32_t place_bits, uint32_t n) {
   sh.key[threadIdx.x] = mine;
@@ -547,10 +547,7 @@ __device__ inline uint64_t least_of_interest(Shared<kTeam> &sh, uint64_t mine, u
     if (threadIdx.x == 0) sh.least = least;
   }
   __syncthreads();
-  const uint64_t least = sh.least;
-  if (mine >= least) sh.hot[atomicAdd(&sh.n_hot, 1u)] = threadIdx.x;
-  __syncthreads();
-  return least;
+  return sh.least;
 }
 
 template <uint32_t kTeam>
@@ -571,15 +568,16 @@ __device__ inline Sums join_sums(Shared<kTeam> &sh, Sums mine, float scale2) {
 }
 
 
-// what is asked for: alternatives too, sums alone, or sums alone of logits of which nothing is kept in the caches
-enum Kind { kWithTop, kSums, kSumsOnce };
+// what is asked for: alternatives too or sums alone; and whether nothing of the logits is kept in the caches
+enum Kind { kWithTop, kWithTopOnce, kSums, kSumsOnce };
+constexpr uint32_t kFewChunks = 4;
 
 // Long rows: a workgroup of kTeam threads per row or part of a row.  Thread t takes the part's chunks t, t + kTeam, t + 2 kTeam, ...
 // kN chunks of a lane are on their way at once.
 template <class T, uint32_t kTeam, uint32_t kN, bool kMask, Kind kKind>
 __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_scores_long(Rows a, Scores out, uint32_t part_chunks, Part VL_GLOBAL *parts, uint64_t VL_GLOBAL *part_keys) {
   __shared__ Shared<kTeam> sh;
-  const uint32_t c0 = blockIdx.x * part_chunks, n_top = kKind == kWithTop ? out.n_top : 0;
+  const uint32_t c0 = blockIdx.x * part_chunks, n_top = kKind <= kWithTopOnce ? out.n_top : 0;
   for (uint32_t r = blockIdx.y; r < a.n_row; r += gridDim.y) {
     const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
     const uint8_t VL_GLOBAL *mask = kMask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
@@ -592,7 +590,8 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
     const uint32_t c1 = min(n_chunk, c0 + part_chunks), c1_full = min(n_full, c1);
     const float given = parts ? kNoLogit : given_logit<T>(a, r, token);
     Sums sums = {kNoLogit, 0.0f, 0.0f};
-    uint32_t place = 0;
+    uint32_t place = 0;        // the chunk that sums.m came from
+    float second = kNoLogit;   // the largest logit of the other chunks
     // kHere chunks of this lane from c on, kTeam apart
     auto add = [&](auto n_of, const float (*x)[T::kElems], uint32_t c) {
       constexpr uint32_t kHere = decltype(n_of)::value;
@@ -604,11 +603,14 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
         for (uint32_t j = 1; j < T::kElems; ++j) b[u] = fmaxf(b[u], x[u][j]);
         m = fmaxf(m, b[u]);
       }
-      if (n_top) {
-        uint32_t first = c + (kHere - 1) * kTeam;
+      if (kKind <= kWithTopOnce) {
+        float best = sums.m;
 #pragma unroll
-        for (uint32_t u = kHere - 1; u-- > 0;) first = b[u] == m ? c + u * kTeam : first;
-        place = m > sums.m ? first : place;
+        for (uint32_t u = 0; u < kHere; ++u) {
+          second = __builtin_amdgcn_fmed3f(best, second, b[u]);   // (second <= best)
+          place = b[u] > best ? c + u * kTeam : place;
+          best = fmaxf(best, b[u]);
+        }
       }
       sums = rebase(sums, fmaxf(sums.m, m), a.scale2);
       const float ref = ref_of(sums.m);
@@ -626,7 +628,7 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
       uint32_t bits[kN];
       if (c - threadIdx.x + kN * kTeam <= c1_full) {
 #pragma unroll
-        for (uint32_t u = 0; u < kN; ++u) w[u] = kKind == kSumsOnce ? load_once<T>(row, lead, c + u * kTeam) : load_even<T>(row, lead, c + u * kTeam);
+        for (uint32_t u = 0; u < kN; ++u) w[u] = kKind == kSumsOnce || kKind == kWithTopOnce ? load_once<T>(row, lead, c + u * kTeam) : load_even<T>(row, lead, c + u * kTeam);
         if (kMask) {
 #pragma unroll
           for (uint32_t u = 0; u < kN; ++u) bits[u] = mask_bits<T>(mask, lead, c + u * kTeam);
@@ -661,25 +663,36 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
     if (!parts) f = finish(a, out, r, sums, given, threadIdx.x == 0);
     else if (threadIdx.x == 0) parts[(uint64_t)r * gridDim.x + blockIdx.x] = Part{sums.m, sums.s, sums.y, 0.0f};
     if (n_top) {
-      const uint64_t least = least_of_interest<T>(sh, mine == kNoLogit ? 0ull : key_of(ordered<T>(mine), place), bits_for(n_chunk), n_top);
-      // the hot lanes' chunks, dealt out to all threads
-      const uint32_t n_hot = sh.n_hot, each = (c1 - c0 + kTeam - 1) / kTeam;
+      const uint64_t key = mine == kNoLogit ? 0ull : key_of(ordered<T>(mine), place), least = least_of_interest<T>(sh, key, bits_for(n_chunk), n_top);
+      const bool hot = key >= least;
+      const uint32_t each = (c1 - c0 + kTeam - 1) / kTeam;
+      const bool own = each > kFewChunks;   // (fewer: all chunks of all hot threads at once)
+      if (hot && !own) sh.hot[atomicAdd(&sh.n_hot, 1u)] = threadIdx.x;
+      if (hot && own) {
+        float x[T::kElems];
+        load_any<T>(a, row, mask, lead, place, x);
+        each_candidate<T>(x, lead, place, least, [&](uint64_t k, bool is) { if (is) gather(sh.room, k); });
+        if (second != kNoLogit && ordered<T>(second) >= (uint32_t)(least >> 32)) sh.hot[atomicAdd(&sh.n_hot, 1u)] = threadIdx.x;
+      }
+      __syncthreads();
+      // the (other) chunks of hot threads that have more to offer, dealt out to all
+      const uint32_t n_hot = sh.n_hot;
       for (uint32_t i = threadIdx.x; i < n_hot * each; i += kTeam) {
-        const uint32_t turn = i / n_hot, at = c0 + sh.hot[i - turn * n_hot] + turn * kTeam;
-        if (at >= c1) continue;
+        const uint32_t turn = i / n_hot, who = sh.hot[i - turn * n_hot], at = c0 + who + turn * kTeam;
+        if (at >= c1 || (own && at == (uint32_t)~sh.key[who])) continue;
         float x[T::kElems];
         load_any<T>(a, row, mask, lead, at, x);
         each_candidate<T>(x, lead, at, least, [&](uint64_t k, bool is) { if (is) gather(sh.room, k); });
       }
-      __syncthreads();
+      if (n_hot) __syncthreads();
       uint64_t best;
       if (sh.room.n <= sh.room.kMost) {
         best = in_order(sh.room.key, sh.room.n, sh.key, n_top);
       } else {
         const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         List list;
-        for (uint32_t h = wave; h < n_hot; h += kTeam / 64) {
-          const uint32_t from = c0 + sh.hot[h];
+        for (uint64_t all = __ballot(hot); all; all &= all - 1) {   // this wavefront's hot threads, all their chunks
+          const uint32_t from = c0 + wave * 64 + (uint32_t)__builtin_ctzll(all);
           for (uint32_t base = from; base < c1; base += 64 * kTeam) {
             const uint32_t at = base + lane * kTeam;
             float x[T::kElems];
@@ -915,7 +928,8 @@ Rows device_rows(const vl_token_rows *a) {
 // rows for all wavefronts, if no alternatives are asked for or the row is short (they are found in a share of the row that
 // falls with the threads); more threads per row the fewer rows there are; and parts, which a second launch joins, where few rows
 // are too long for one workgroup.  Measured, us (this choice / the other):
-//   3,000 x 5,000, no alternatives: 64 threads 10.5 / 256 13.2;      4,096 x 50,000, five: 256 90 / 64 119
+//   3,000 x 5,000, no alternatives: 64 threads 10.5 / 256 13.2;      4,096 x 20,000, twenty: 64 46 / 256 48
+//   (4,096 x 50,001 in 32 bits, five, 12,501 chunks: 256 73.7 / 64 77.4)
 //   500 x 32,000 in 32 bits: 1,024 in 1 part 17.7 / 256 in 4 24.0;   300 x 50,001: 1,024 17.8 / 256 in 5 20.7
 //   1 x 32,000: 1,024 in 1 part 9.4 / 256 in 7 11.6;                 1 x 131,072: 256 in 32 parts 11.9 / 1,024 in 1 15.3
 //   1 x 5,000: 256 6.9 / 1,024 9.3;                                  100 x 131,072: 1,024 in 1 part 16.2 / in 5 17.6
@@ -924,7 +938,7 @@ Split split_of(const vl_token_rows *a, uint32_t n_top) {
   const uint32_t n = most_chunks_of(a), rows = a->n_row;
   const bool few = rows < 128;
   uint32_t team = 1024, parts = 1;
-  if (rows >= 2048 && (n_top == 0 || n <= 2048)) team = 64;
+  if (rows >= 2048 && (n_top == 0 || n <= 8192)) team = 64;
   else if (rows >= 1024 || (few && n <= 1024)) team = 256;
   else if (!few) parts = std::max(1u, std::min(512 / rows, n / 1024));
   else if (rows < 48 && n > 8192) { team = 256; parts = std::min({2048 / rows, n / 512, 256u}); }
@@ -942,11 +956,18 @@ template <class T, uint32_t kTeam, uint32_t kN>
 void launch_long(const Rows &a, const Scores &out, Split split, Part VL_GLOBAL *parts, uint64_t VL_GLOBAL *keys, hipStream_t stream) {
   const dim3 grid(split.parts, std::min(a.n_row, kMostGridY));
   // Logits beyond what the Infinity Cache holds (256 MB) are not kept in the caches: 1,500 rows of 131,072 77 -> 69 us,
-  // 8,000 of 20,000 65 -> 56; but 64 MB that the program before has just written 17.7 -> 19.9.  With alternatives, whose chunks are read
-  // again, it makes no difference (4,096 x 50,001 and five of them: 89).
-  const bool once = (uint64_t)a.n_row * a.n_vocab * sizeof(typename T::type) > (256ull << 20);
-  (a.mask ? out.n_top ? k_scores_long<T, kTeam, kN, true, kWithTop> : once ? k_scores_long<T, kTeam, kN, true, kSumsOnce> : k_scores_long<T, kTeam, kN, true, kSums>
-          : out.n_top ? k_scores_long<T, kTeam, kN, false, kWithTop> : once ? k_scores_long<T, kTeam, kN, false, kSumsOnce> : k_scores_long<T, kTeam, kN, false, kSums>)
+  // 8,000 of 20,000 65 -> 56, with five alternatives 4,096 of 50,001 85 -> 82; but 64 MB that the program before has just written
+  // 17.7 -> 19.9.
+  if constexpr (kTeam != 1024 || kN != 4) {   // (fewer than 128 rows are never that much)
+    if ((uint64_t)a.n_row * a.n_vocab * sizeof(typename T::type) > (256ull << 20)) {
+      (a.mask ? out.n_top ? k_scores_long<T, kTeam, kN, true, kWithTopOnce> : k_scores_long<T, kTeam, kN, true, kSumsOnce>
+              : out.n_top ? k_scores_long<T, kTeam, kN, false, kWithTopOnce> : k_scores_long<T, kTeam, kN, false, kSumsOnce>)
+          <<<grid, kTeam, 0, stream>>>(a, out, split.chunks, parts, keys);
+      return;
+    }
+  }
+  (a.mask ? out.n_top ? k_scores_long<T, kTeam, kN, true, kWithTop> : k_scores_long<T, kTeam, kN, true, kSums>
+          : out.n_top ? k_scores_long<T, kTeam, kN, false, kWithTop> : k_scores_long<T, kTeam, kN, false, kSums>)
       <<<grid, kTeam, 0, stream>>>(a, out, split.chunks, parts, keys);
 }
 template <class T>
