@@ -275,16 +275,25 @@ __device__ inline uint64_t lane_key(uint64_t k, uint32_t lane) {
   return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
 }
 
+__device__ inline uint32_t lanes_below(uint64_t lanes) {   // how many of them are below this one
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0));
+}
+
 // A number that at least n of the keys which a wavefront's lanes hold (0: none, the others all differ) reach, and at
 // most `most` >= n of them; 1 if there are fewer than n.  Bit by bit from the top; places are below 2^place_bits.
 template <uint32_t kBits>
 __device__ inline uint64_t nth_key(uint64_t k, uint32_t place_bits, uint32_t n, uint32_t most) {
-  uint32_t value = 0;
-  for (int32_t bit = kBits - 1; bit >= 0; --bit) {
-    const uint32_t attempt = value | (1u << bit), count = __popcll(__ballot((uint32_t)(k >> 32) >= attempt));
-    if (count < n) continue;
-    value = attempt;
-    if (count <= most) return (uint64_t)value << 32;
+  // (four bits at a time without a branch: one scalar unit serves a compute unit's wavefronts)
+  uint32_t value = 0, reached = 0;
+#pragma unroll
+  for (int32_t top = kBits - 1; top >= 0; top -= 4) {
+#pragma unroll
+    for (int32_t bit = top; bit > top - 4 && bit >= 0; --bit) {
+      const uint32_t attempt = value | (1u << bit), count = __popcll(__ballot((uint32_t)(k >> 32) >= attempt));
+      value = count >= n ? attempt : value;
+      reached = count >= n ? count : reached;
+    }
+    if (reached && reached <= most) return (uint64_t)value << 32;
   }
   if (!value) return 1ull;
   uint64_t least = ((uint64_t)value << 32) | (0xFFFFFFFFull & ~((1ull << place_bits) - 1ull));   // (the same in every key)
@@ -333,15 +342,14 @@ struct List {
   }
 };
 
-// f(key) for those of a chunk's logits that are at or above `least`, a (value, chunk), and so may be among the best
+// f(is, key) for a chunk's logits, `is` set for those at or above `least`, a (value, chunk), which so may be among the best; key() makes
+// the number
 template <class T, class F>
 __device__ inline void each_candidate(const float *x, uint32_t lead, uint32_t c, uint64_t least, F f) {
   const uint32_t value = (uint32_t)(least >> 32) + (c <= (uint32_t)~least ? 0u : 1u);
+  const float from = value <= (0x00800000u >> (32 - T::kBits)) ? kLeast : unordered<T>(value);   // (any but -infinity, at the least)
 #pragma unroll
-  for (uint32_t j = 0; j < T::kElems; ++j) {
-    const uint32_t u = ordered<T>(x[j]);
-    f(key_of(u, c * T::kElems - lead + j), x[j] != kNoLogit && u >= value);
-  }
+  for (uint32_t j = 0; j < T::kElems; ++j) f(x[j] >= from, [&] { return key_of(ordered<T>(x[j]), c * T::kElems - lead + j); });
 }
 
 // ---- what a row's results are made of
@@ -476,11 +484,11 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
       uint32_t found = 0;
 #pragma unroll
       for (uint32_t i = 0; i < kChunks; ++i)
-        each_candidate<T>(x[i], 0, lane + 64 * i, least, [&](uint64_t k, bool is) {
+        each_candidate<T>(x[i], 0, lane + 64 * i, least, [&](bool is, auto key_at) {
           const uint64_t all = __ballot(is);
           if (!all) return;
-          const uint32_t at = found + __popcll(all & ((1ull << lane) - 1ull));
-          if (is && at < 64) room[wave][at] = k;
+          const uint32_t at = found + lanes_below(all);
+          if (is && at < 64) room[wave][at] = key_at();
           found += __popcll(all);
         });
       if (found <= 64) {
@@ -494,7 +502,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
         List list;
 #pragma unroll
         for (uint32_t i = 0; i < kChunks; ++i)
-          each_candidate<T>(x[i], 0, lane + 64 * i, least, [&](uint64_t k, bool is) { list.insert_lanes(k, is, n); });
+          each_candidate<T>(x[i], 0, lane + 64 * i, least, [&](bool is, auto key_at) { list.insert_lanes(key_at(), is, n); });
         if (lane < n) write_top<T>(out, r, lane, list.key, f);
       }
     }
@@ -671,7 +679,7 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
       if (hot && own) {
         float x[T::kElems];
         load_any<T>(a, row, mask, lead, place, x);
-        each_candidate<T>(x, lead, place, least, [&](uint64_t k, bool is) { if (is) gather(sh.room, k); });
+        each_candidate<T>(x, lead, place, least, [&](bool is, auto key_at) { if (is) gather(sh.room, key_at()); });
         if (second != kNoLogit && ordered<T>(second) >= (uint32_t)(least >> 32)) sh.hot[atomicAdd(&sh.n_hot, 1u)] = threadIdx.x;
       }
       __syncthreads();
@@ -682,7 +690,7 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
         if (at >= c1 || (own && at == (uint32_t)~sh.key[who])) continue;
         float x[T::kElems];
         load_any<T>(a, row, mask, lead, at, x);
-        each_candidate<T>(x, lead, at, least, [&](uint64_t k, bool is) { if (is) gather(sh.room, k); });
+        each_candidate<T>(x, lead, at, least, [&](bool is, auto key_at) { if (is) gather(sh.room, key_at()); });
       }
       if (n_hot) __syncthreads();
       uint64_t best;
@@ -702,7 +710,7 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
 #pragma unroll
               for (uint32_t j = 0; j < T::kElems; ++j) x[j] = kNoLogit;
             }
-            each_candidate<T>(x, lead, at, least, [&](uint64_t k, bool is) { list.insert_lanes(k, is, n_top); });
+            each_candidate<T>(x, lead, at, least, [&](bool is, auto key_at) { list.insert_lanes(key_at(), is, n_top); });
           }
         }
         best = join_lists(sh, list, n_top);
