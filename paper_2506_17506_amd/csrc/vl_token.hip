@@ -308,6 +308,15 @@ __device__ inline uint64_t nth_key(uint64_t k, uint32_t place_bits, uint32_t n, 
 }
 __device__ inline uint32_t bits_for(uint32_t n) { return 32u - (uint32_t)__builtin_clz(n | 1u); }   // of numbers up to n
 
+// how many of the first `found` keys are larger; the list goes on with zeros to a multiple of four
+__device__ inline uint32_t rank_of(const uint64_t *keys, uint32_t found, uint64_t mine) {
+  uint32_t rank = 0;
+  for (uint32_t i = 0; i < found; i += 4)
+#pragma unroll
+    for (uint32_t u = 0; u < 4; ++u) rank += keys[i + u] > mine;
+  return rank;
+}
+
 // Where keys that may be among a row's n best are gathered.  More than there is room for are possible (many equal
 // logits, or a row sorted in an unlucky way); then the row's best are found by insertion instead.
 constexpr uint32_t kMoreHot = 4;   // more than n lanes may have their chunks looked at again, so that the search for them ends sooner
@@ -482,6 +491,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
       const uint64_t least = nth_key<T::kBits>(key, bits_for(64 * kChunks - 1), n, n + kMoreHot);
       // gathered in the order of the lanes; up to 64 of them, usual unless many are equal, one per lane
       uint32_t found = 0;
+      room[wave][lane] = 0;
 #pragma unroll
       for (uint32_t i = 0; i < kChunks; ++i)
         each_candidate<T>(x[i], 0, lane + 64 * i, least, [&](bool is, auto key_at) {
@@ -493,9 +503,8 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
         });
       if (found <= 64) {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");   // (written and read by one wavefront)
-        const uint64_t mine = lane < found ? room[wave][lane] : 0ull;
-        uint32_t rank = 0;
-        for (uint32_t i = 0; i < found; ++i) rank += lane_key(mine, i) > mine;
+        const uint64_t mine = room[wave][lane];
+        const uint32_t rank = rank_of(room[wave], found, mine);
         if (lane < found && rank < n) write_top<T>(out, r, rank, mine, f);
         if (lane >= found && lane < n) write_top<T>(out, r, lane, 0, f);
       } else {
@@ -517,18 +526,19 @@ struct Shared {
   Sums sums[kTeam / 64];
   Room<kTeam> room;
   uint64_t key[kTeam < 64 ? 64 : kTeam];
-  uint64_t list[kTeam / 64 * VL_MAX_TOP];
+  uint64_t list[kTeam / 64 * VL_MAX_TOP];   // (a multiple of four long)
   uint64_t least;
   uint32_t n_hot, hot[kTeam];
 };
 
-// The n best of `found` different keys, no more than there are threads, best first: entry k in thread k < n, 0 where there are fewer
+// The n best of `found` different keys, no more than there are threads, best first: entry k in thread k < n, 0 where there are fewer.  (Lists
+// for rank_of: the wavefronts' lists are 4 n or 16 n keys, a single one n and zeros.)
 __device__ inline uint64_t in_order(const uint64_t *keys, uint32_t found, uint64_t *out, uint32_t n) {
   const uint64_t mine = threadIdx.x < found ? keys[threadIdx.x] : 0ull;
-  uint32_t rank = 0;
-  if (threadIdx.x < found)
-    for (uint32_t i = 0; i < found; ++i) rank += keys[i] > mine;
-  if (threadIdx.x < found && mine && rank < n) out[rank] = mine;
+  if (threadIdx.x < found && mine) {
+    const uint32_t rank = rank_of(keys, found, mine);
+    if (rank < n) out[rank] = mine;
+  }
   __syncthreads();
   return threadIdx.x < n && threadIdx.x < found ? out[threadIdx.x] : 0ull;
 }
@@ -537,6 +547,7 @@ template <uint32_t kTeam>
 __device__ inline uint64_t join_lists(Shared<kTeam> &sh, const List &list, uint32_t n) {
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
   if (lane < n) sh.list[wave * n + lane] = list.key;
+  if (kTeam == 64 && lane >= n && lane < VL_MAX_TOP) sh.list[lane] = 0;
   if (threadIdx.x < n) sh.key[threadIdx.x] = 0;   // (done with by now)
   __syncthreads();
   return in_order(sh.list, kTeam / 64 * n, sh.key, n);
@@ -545,6 +556,7 @@ __device__ inline uint64_t join_lists(Shared<kTeam> &sh, const List &list, uint3
 template <class T, uint32_t kTeam>
 __device__ inline uint64_t least_of_interest(Shared<kTeam> &sh, uint64_t mine, uint32_t place_bits, uint32_t n) {
   sh.key[threadIdx.x] = mine;
+  if (threadIdx.x < sh.room.kMost) sh.room.key[threadIdx.x] = 0;
   if (threadIdx.x == 0) sh.n_hot = sh.room.n = 0;
   __syncthreads();
   if (threadIdx.x < 64) {   // of several threads' best the best one: a key that n of these 64 reach serves as well
