@@ -341,8 +341,8 @@ typedef struct {
 } vl_mask_query;
 int32_t vl_free_bases_multi(const vl_mask_query *queries, uint32_t n, uint32_t *masks, vl_stream stream);
 
-/* Token scores: what a program computes from the logits of the model that answers (Section 3.1
- * trains it by cross entropy, Section 3.4 samples it, Section 6 proposes the verifier as its
+/* Token scores: what a program computes from the logits of the model that answers (Equations 1 and
+ * 2 train it by cross entropy, Section 3.4 samples it, Section 6 proposes the verifier as its
  * reward).  A row is the logits of one token that was or is to be emitted, over n_vocab tokens;
  * where a token stands for a register, a window of the vocabulary is a row as well: logits points
  * at the window's first token, ld stays the whole vocabulary's, and the words that
