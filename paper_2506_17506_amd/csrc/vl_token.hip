@@ -502,7 +502,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
           found += __popcll(all);
         });
       if (found <= 64) {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");   // (written and read by one wavefront)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (written and read by one wavefront)
         const uint64_t mine = room[wave][lane];
         const uint32_t rank = rank_of(room[wave], found, mine);
         if (lane < found && rank < n) write_top<T>(out, r, rank, mine, f);
@@ -915,7 +915,11 @@ constexpr uint32_t kMostGridY = 65535;
 
 uint32_t size_of(uint32_t type) { return type == VL_F32 ? 4u : 2u; }
 uint32_t chunks_of(const vl_token_rows *a) { const uint32_t e = 16u / size_of(a->type); return (a->n_vocab + e - 1) / e; }
-uint32_t most_chunks_of(const vl_token_rows *a) { const uint32_t e = 16u / size_of(a->type); return (a->n_vocab + (e == 8) + e - 1) / e; }   // (a lead included)
+uint32_t most_chunks_of(const vl_token_rows *a) {   // of a row with its lead, if some row has one
+  const bool lead = a->type != VL_F32 && (((uintptr_t)a->logits & 2) || (a->n_row > 1 && (a->ld & 1)));
+  const uint32_t e = 16u / size_of(a->type);
+  return (a->n_vocab + lead + e - 1) / e;
+}
 
 int32_t check_rows(const vl_token_rows *a) {
   if (!a || !a->logits) return VL_E_NULL;
@@ -951,7 +955,7 @@ Rows device_rows(const vl_token_rows *a) {
 //   3,000 x 5,000, no alternatives: 64 threads 10.5 / 256 13.2;      4,096 x 20,000, twenty: 64 46 / 256 48
 //   (4,096 x 50,001 in 32 bits, five, 12,501 chunks: 256 73.7 / 64 77.4)
 //   500 x 32,000 in 32 bits: 1,024 in 1 part 17.7 / 256 in 4 24.0;   300 x 50,001: 1,024 17.8 / 256 in 5 20.7
-//   1 x 32,000: 1,024 in 1 part 9.4 / 256 in 7 11.6;                 1 x 131,072: 256 in 32 parts 11.9 / 1,024 in 1 15.3
+//   1 x 32,000: 1,024 in 1 part 9.4 / 256 in 7 11.6;                 1 x 131,072: 256 in 21 parts 10.2 / in 32 10.6, 1,024 in 1 15.3
 //   1 x 5,000: 256 6.9 / 1,024 9.3;                                  100 x 131,072: 1,024 in 1 part 16.2 / in 5 17.6
 struct Split { uint32_t team, parts, chunks; bool few; };   // few: a compute unit has one workgroup at most, which may use twice the registers
 Split split_of(const vl_token_rows *a, uint32_t n_top) {
@@ -961,7 +965,7 @@ Split split_of(const vl_token_rows *a, uint32_t n_top) {
   if (rows >= 2048 && (n_top == 0 || n <= 8192)) team = 64;
   else if (rows >= 1024 || (few && n <= 1024)) team = 256;
   else if (!few) parts = std::max(1u, std::min(512 / rows, n / 1024));
-  else if (rows < 48 && n > 8192) { team = 256; parts = std::min({2048 / rows, n / 512, 256u}); }
+  else if (rows < 48 && n > 8192) { team = 256; parts = std::min({2048 / rows, n / 768, 256u}); }
   if (parts == 1) return Split{team, 1, n, few};
   const uint32_t chunks = ((n + parts - 1) / parts + team - 1) / team * team;
   return Split{team, (n + chunks - 1) / chunks, chunks, few};

@@ -178,7 +178,7 @@ def test_odd_rows(v, dtype, scale):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
-@pytest.mark.parametrize("n,v", [(3, 512), (3, 515), (2, 9000), (300, 700)])
+@pytest.mark.parametrize("n,v", [(3, 512), (3, 515), (2, 9000), (300, 700), (1, 131072), (2, 98304), (2, 70001), (1100, 1040), (2100, 1041)])
 @pytest.mark.parametrize("first,after", [(1, 0), (3, 5), (8, 8), (13, 0)])
 def test_windows_of_wider_rows(dtype, n, v, first, after):
     """logits and gradient in rows of another pitch and start; what lies beside them stays, and is not looked at"""
