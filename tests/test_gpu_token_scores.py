@@ -28,6 +28,8 @@ def scores(x, token=None, mask=None, scale=1.0, top=0, stream=None):
     if top:
         out["top_token"] = torch.full((n, top), 77, dtype=torch.int32, device="cuda")
         out["top_logprob"] = torch.full((n, top), 7.0, device="cuda")
+    if stream is not None:
+        torch.cuda.synchronize()   # (the presets are another stream's work)
     vl.vl_token_logprobs(x, token=token, mask=mask, scale=scale, stream=stream, **out)
     return out
 
@@ -316,11 +318,15 @@ def test_two_streams_and_a_recorded_pass():
     wants = [Rows(x, t, top=8) for x, t in zip(xs, ts)]
     streams = [torch.cuda.Stream() for _ in range(2)]
     torch.cuda.synchronize()
-    outs = [[], []]
+
+    def room():
+        return dict(logprob=torch.full((n,), 7.0, device="cuda"), entropy=torch.full((n,), 7.0, device="cuda"), stat=torch.full((n, 2), 7.0, device="cuda"),
+                    top_token=torch.full((n, 8), 77, dtype=torch.int32, device="cuda"), top_logprob=torch.full((n, 8), 7.0, device="cuda"))
+    outs = [[room() for _ in range(6)] for _ in range(2)]
+    torch.cuda.synchronize()
     for turn in range(6):
         for k in range(2):
-            with torch.cuda.stream(streams[k]) if turn % 2 else torch.cuda.stream(torch.cuda.current_stream()):
-                outs[k].append(scores(xs[k], ts[k], top=8, stream=streams[k]))
+            vl.vl_token_logprobs(xs[k], token=ts[k], stream=streams[k], **outs[k][turn])
     torch.cuda.synchronize()
     for k in range(2):
         for o in outs[k]:
@@ -335,6 +341,7 @@ def test_two_streams_and_a_recorded_pass():
         vl.vl_token_logprobs(x, token=t, **out)
         vl.vl_token_logprobs_grad(x, out["stat"], grad, token=t, g_logprob=g_dev)
     side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         one_pass()
     torch.cuda.synchronize()
@@ -401,6 +408,19 @@ def test_refusals_of_the_binding():
         assert err.value.code == want
     torch.cuda.synchronize()
     assert (out == 0).all()
+
+
+def test_forms_of_a_stream():
+    """a torch stream, its handle as a number, the default stream as None and as 0, a ctypes pointer"""
+    import ctypes
+    x, t = bell(2, 131072, BF16, 1), tokens(2, 131072, 2)
+    want = Rows(x, t, top=4)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (None, 0, torch.cuda.current_stream(), side, side.cuda_stream, ctypes.c_void_p(side.cuda_stream), ctypes.c_void_p(0)):
+        out = scores(x, t, top=4, stream=stream)
+        torch.cuda.synchronize()
+        check_scores(out, want, str(stream))
 
 
 def test_work_of_the_callers():
