@@ -388,7 +388,7 @@ typedef struct {        /* every pointer is [device] and may be NULL, not all of
 } vl_token_scores;
 /* Asynchronous on `stream`: enqueues kernels only, keeps nothing between calls.  work [device]: the caller's memory for
  * the parts of rows that are shared among workgroups, on a 16-byte boundary, of at least the bytes that
- * vl_token_logprobs_work says for the same arguments (0 for most: work may then be NULL); its contents need not be
+ * vl_token_logprobs_work says for the same sizes, type and n_top (0 for most: work may then be NULL); its contents need not be
  * kept or cleared, but calls that may overlap need one each, recorded ones included.
  * Errors: VL_E_NULL, VL_E_SHAPE (a size, pitch or alignment), VL_E_RANGE (n_vocab, type, scale, n_top, reserved0);
  * nothing is launched on error. */

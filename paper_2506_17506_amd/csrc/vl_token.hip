@@ -914,11 +914,9 @@ constexpr uint32_t kShortGradChunks = 256;
 constexpr uint32_t kMostGridY = 65535;
 
 uint32_t size_of(uint32_t type) { return type == VL_F32 ? 4u : 2u; }
-uint32_t chunks_of(const vl_token_rows *a) { const uint32_t e = 16u / size_of(a->type); return (a->n_vocab + e - 1) / e; }
-uint32_t most_chunks_of(const vl_token_rows *a) {   // of a row with its lead, if some row has one
-  const bool lead = a->type != VL_F32 && (((uintptr_t)a->logits & 2) || (a->n_row > 1 && (a->ld & 1)));
-  const uint32_t e = 16u / size_of(a->type);
-  return (a->n_vocab + lead + e - 1) / e;
+uint32_t chunks_of(const vl_token_rows *a, bool lead = false) { const uint32_t e = 16u / size_of(a->type); return (a->n_vocab + lead + e - 1) / e; }
+bool has_lead(const vl_token_rows *a) {   // some row starts at an odd place
+  return a->type != VL_F32 && (((uintptr_t)a->logits & 2) || (a->n_row > 1 && (a->ld & 1)));
 }
 
 int32_t check_rows(const vl_token_rows *a) {
@@ -958,8 +956,8 @@ Rows device_rows(const vl_token_rows *a) {
 //   1 x 32,000: 1,024 in 1 part 9.4 / 256 in 7 11.6;                 1 x 131,072: 256 in 21 parts 10.2 / in 32 10.6, 1,024 in 1 15.3
 //   1 x 5,000: 256 6.9 / 1,024 9.3;                                  100 x 131,072: 1,024 in 1 part 16.2 / in 5 17.6
 struct Split { uint32_t team, parts, chunks; bool few; };   // few: a compute unit has one workgroup at most, which may use twice the registers
-Split split_of(const vl_token_rows *a, uint32_t n_top) {
-  const uint32_t n = most_chunks_of(a), rows = a->n_row;
+Split split_of(const vl_token_rows *a, uint32_t n_top, bool lead) {
+  const uint32_t n = chunks_of(a, lead), rows = a->n_row;
   const bool few = rows < 128;
   uint32_t team = 1024, parts = 1;
   if (rows >= 2048 && (n_top == 0 || n <= 8192)) team = 64;
@@ -972,8 +970,9 @@ Split split_of(const vl_token_rows *a, uint32_t n_top) {
 }
 uint64_t work_of(const vl_token_rows *a, const vl_token_scores *o) {
   if (chunks_of(a) <= kShortChunks) return 0;
-  const Split s = split_of(a, o->n_top);
-  return s.parts == 1 ? 0 : (uint64_t)a->n_row * s.parts * (sizeof(Part) + 8ull * o->n_top);
+  // enough wherever the rows start
+  const uint32_t parts = std::max(split_of(a, o->n_top, false).parts, split_of(a, o->n_top, a->type != VL_F32).parts);
+  return parts == 1 ? 0 : (uint64_t)a->n_row * parts * (sizeof(Part) + 8ull * o->n_top);
 }
 
 template <class T, uint32_t kTeam, uint32_t kN>
@@ -1046,7 +1045,7 @@ extern "C" int32_t vl_token_logprobs(const vl_token_rows *rows, const vl_token_s
   const Scores o = {(float VL_GLOBAL *)out->logprob, (float VL_GLOBAL *)out->entropy, (float VL_GLOBAL *)out->stat, (float VL_GLOBAL *)out->top_logprob,
                     (int32_t VL_GLOBAL *)out->top_token, out->n_top};
   (rows->type == VL_F32 ? launch_scores<F32> : rows->type == VL_F16 ? launch_scores<F16> : launch_scores<BF16>)(
-      device_rows(rows), o, chunks_of(rows), split_of(rows, out->n_top), work, stream);
+      device_rows(rows), o, chunks_of(rows), split_of(rows, out->n_top, has_lead(rows)), work, stream);
   VL_HIP(hipGetLastError());
   return VL_OK;
 }

@@ -7,11 +7,11 @@ from stand_in import in_own_process
 P = 1 << 20   # a pointer that nothing follows
 
 
-def _scores(s, n, v, kind, top, mask=True, ld=None, stream=0x77):
+def _scores(s, n, v, kind, top, mask=True, ld=None, odd=0, stream=0x77):
     """(launches, work bytes) of one call"""
     from paper_2506_17506_amd import binding as b
     lib = s.vl.load()
-    rows = b._TokenRows(P, ld or v, P if mask else None, (v + 31) // 32 if mask else 0, P, n, v, kind, 1.0)
+    rows = b._TokenRows(P + odd, ld or v, P if mask else None, (v + 31) // 32 if mask else 0, P, n, v, kind, 1.0)
     out = b._TokenScores(P, P, P, P if top else None, P if top else None, top, 0)
     need = C.c_uint64()
     assert lib.vl_token_logprobs_work(C.byref(rows), C.byref(out), C.byref(need)) == 0
@@ -31,7 +31,9 @@ def test_scores_launch_kernels_only_and_cover_their_rows(s):
         for kind in (0, 1, 2):
             top = rng.choice([0, 0, 1, 20, 32])
             ld = v + rng.choice([0, 0, 1, 64])
-            launches, need = _scores(s, n, v, kind, top, mask=rng.random() < 0.5, ld=ld)
+            launches, need = _scores(s, n, v, kind, top, mask=rng.random() < 0.5, ld=ld, odd=0 if kind == 0 else rng.choice([0, 0, 2]))
+            other = _scores(s, n, v, kind, top, ld=v + 1, odd=0 if kind == 0 else 2)[1]
+            assert need == other, (n, v, kind, top, need, other)
             assert 1 <= len(launches) <= 2 and all(x[4] == 0x77 for x in launches)
             for name, grid, block, lds, stream, words in launches:
                 assert all(1 <= g for g in grid) and grid[0] * block < 2 ** 32 and grid[1] <= 65535 and grid[2] == 1, (n, v, kind, name, grid)
@@ -40,7 +42,8 @@ def test_scores_launch_kernels_only_and_cover_their_rows(s):
                 assert grid[1] == min(n, 65535)
                 parts = grid[0]
                 assert (parts > 1) == (len(launches) == 2) and parts <= 256, (n, v, grid)
-                assert need == (n * parts * (16 + 8 * top) if parts > 1 else 0), (n, v, need, grid)
+                least = n * parts * (16 + 8 * top) if parts > 1 else 0
+                assert least <= need <= n * 256 * (16 + 8 * top), (n, v, need, grid)   # (it does not go by where the rows start)
                 if parts > 1:
                     assert "k_scores_join" in launches[1][0] and launches[1][1][0] == n and launches[1][2] == 256
             else:
