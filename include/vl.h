@@ -437,10 +437,10 @@ int32_t vl_group_advantages(const vl_counts *counts, const float *extra, uint32_
  * bounds in 64 bits; sums are joined in 64 bits in an order that the sizes alone decide.  grad is written at the samples'
  * tokens only and may be logprob itself.  Tokens at n or above are not touched, and stats->n_token leaves them out.
  * max_len: the longest sample, as near as the host knows it: it decides the launch's shape alone.
- * work [device]: memory of the caller as for vl_token_logprobs, at least vl_policy_loss_work bytes.
+ * work [device]: memory of the caller as for vl_token_logprobs, at least vl_policy_loss_work bytes (0 for few tokens).
  * Asynchronous on `stream`, enqueues kernels only.
- * Errors: VL_E_NULL (kl != 0 without logprob_ref among them), VL_E_SHAPE (n or n_sample is 0, n_sample 2^31 or more, a pointer not aligned to its
- * elements, work too small), VL_E_RANGE (log_lo > log_hi or one of them NaN, kl not finite); nothing is launched on error. */
+ * Errors: VL_E_NULL (kl != 0 without logprob_ref among them), VL_E_SHAPE (n or n_sample is 0, n 2^60 or more, n_sample 2^31 or more, a
+ * pointer not aligned to its elements, work too small or not on a 16-byte boundary), VL_E_RANGE (log_lo > log_hi or one of them NaN, kl not finite); nothing is launched on error. */
 typedef struct {
   const float *logprob, *logprob_old, *logprob_ref; /* [device] [n]; logprob_ref may be NULL */
   uint64_t n;

@@ -114,7 +114,6 @@ struct Batch {
 };
 struct Part { double loss, kl; uint64_t n_token, n_clipped; };
 
-constexpr uint32_t kPolicyThreads = 256, kPolicyWaves = kPolicyThreads / 64;
 constexpr uint32_t kGroups = 2, kStep = kGroups * 256;   // a lane takes kGroups times four tokens, a wavefront kStep, at once
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
@@ -136,11 +135,19 @@ struct Sample { uint64_t from, to; float a, w; };
 
 // A wavefront takes a slice of a sample at a time.  What bounds it: the arrays' bytes.  Whether d is past a bound is decided in 64
 // bits, where the difference of two numbers of 32 is exact (unless they are so far apart that no rounding matters), and every loss goes into a sum of 64 bits.
-template <bool kRef>
-__global__ __launch_bounds__(kPolicyThreads) void k_policy(Batch b, Part VL_GLOBAL *parts) {
-  __shared__ Part room[kPolicyWaves];
+__device__ inline Part add_parts(Part p, const Part &q) { return Part{p.loss + q.loss, p.kl + q.kl, p.n_token + q.n_token, p.n_clipped + q.n_clipped}; }
+__device__ inline void write_stats(vl_policy_stats VL_GLOBAL *stats, const Part &p) {
+  stats->loss = (float)p.loss;
+  stats->kl = (float)p.kl;
+  stats->n_token = p.n_token;
+  stats->n_clipped = p.n_clipped;
+}
+
+template <bool kRef, uint32_t kWaves>
+__global__ __launch_bounds__(kWaves * 64) void k_policy(Batch b, Part VL_GLOBAL *parts, vl_policy_stats VL_GLOBAL *stats) {
+  __shared__ Part room[kWaves];
   const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t n_unit = (uint64_t)b.n_sample * b.slices, stride = (uint64_t)gridDim.x * kPolicyWaves;
+  const uint64_t n_unit = (uint64_t)b.n_sample * b.slices, stride = (uint64_t)gridDim.x * kWaves;
   double loss = 0, kls = 0;
   uint64_t tokens = 0, clips = 0;
   auto sample_of = [&](uint64_t unit) {
@@ -151,7 +158,7 @@ __global__ __launch_bounds__(kPolicyThreads) void k_policy(Batch b, Part VL_GLOB
     const uint64_t from = least_of(base + slice * per, i1), to = least_of(base + (slice + 1) * per, i1);
     return Sample{from < i0 ? i0 : from, to < i0 ? i0 : to, b.advantage[c], b.weight[c]};
   };
-  for (uint64_t unit = (uint64_t)blockIdx.x * kPolicyWaves + wave; unit < n_unit; unit += stride) {
+  for (uint64_t unit = (uint64_t)blockIdx.x * kWaves + wave; unit < n_unit; unit += stride) {
     const Sample s = sample_of(unit);
     const float bound = s.a > 0.0f ? b.log_hi : b.log_lo;
     const double hi = s.a > 0.0f ? (double)b.log_hi : (double)__builtin_huge_valf(), lo = s.a < 0.0f ? (double)b.log_lo : -(double)__builtin_huge_valf();
@@ -220,8 +227,10 @@ __global__ __launch_bounds__(kPolicyThreads) void k_policy(Batch b, Part VL_GLOB
   __syncthreads();
   if (threadIdx.x == 0) {
     Part all = room[0];
-    for (uint32_t w = 1; w < kPolicyWaves; ++w) {
-      all.loss += room[w].loss; all.kl += room[w].kl; all.n_token += room[w].n_token; all.n_clipped += room[w].n_clipped;
+    for (uint32_t w = 1; w < kWaves; ++w) all = add_parts(all, room[w]);
+    if (gridDim.x == 1) {   // nothing to join
+      write_stats(stats, all);
+      return;
     }
     parts[blockIdx.x].loss = all.loss;
     parts[blockIdx.x].kl = all.kl;
@@ -229,8 +238,6 @@ __global__ __launch_bounds__(kPolicyThreads) void k_policy(Batch b, Part VL_GLOB
     parts[blockIdx.x].n_clipped = all.n_clipped;
   }
 }
-
-__device__ inline Part add_parts(Part p, const Part &q) { return Part{p.loss + q.loss, p.kl + q.kl, p.n_token + q.n_token, p.n_clipped + q.n_clipped}; }
 
 constexpr uint32_t kJoinThreads = 1024;
 __global__ __launch_bounds__(kJoinThreads) void k_policy_join(const Part VL_GLOBAL *parts, uint32_t n, vl_policy_stats VL_GLOBAL *stats) {
@@ -256,12 +263,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_policy_join(const Part VL_GLOB
 #pragma unroll
   for (int d = 8; d; d >>= 1)
     p = add_parts(p, Part{__shfl_xor(p.loss, d), __shfl_xor(p.kl, d), __shfl_xor(p.n_token, d), __shfl_xor(p.n_clipped, d)});
-  if (threadIdx.x == 0) {
-    stats->loss = (float)p.loss;
-    stats->kl = (float)p.kl;
-    stats->n_token = p.n_token;
-    stats->n_clipped = p.n_clipped;
-  }
+  if (threadIdx.x == 0) write_stats(stats, p);
 }
 
 int32_t check_batch(const vl_policy_batch *b) {
@@ -276,12 +278,18 @@ int32_t check_batch(const vl_policy_batch *b) {
 // Slices of a sample, of about 2,048 tokens by the longest one, less where that leaves wavefronts idle, and workgroups for them,
 // 8,192 at most.  (1,600 samples of 43,000 tokens on average, a slice per wavefront: 163 us; 2,048 workgroups that
 // take a slice after the other 173, slices of 4,096 tokens 168, of 1,024 179.)
-struct Launch { uint32_t slices, blocks; };
+// A workgroup of 1,024 threads alone, with nothing to join, takes what is small: two slices per wavefront at most.  (Four
+// samples, us alone / joined: 1,000 tokens 5.4 / 8.4, 16,000 7.6 / 9.0, 32,000 13.0 / 9.2; 100 samples of 1,000 in all 15.9 / 8.5.)
+constexpr uint32_t kAloneTokens = 16384, kAloneSlices = 32;
+struct Launch { uint32_t slices, waves, blocks; };
 Launch launch_of(const vl_policy_batch *b) {
   const uint64_t want = std::max<uint64_t>({1, b->max_len / 2048, std::min<uint64_t>(b->max_len / kStep, 8192 / b->n_sample)}), most = std::max<uint64_t>(1, 0xFFFFFFFFull / b->n_sample);
   const uint32_t slices = (uint32_t)std::min({want, most, (uint64_t)1024});
-  return Launch{slices, (uint32_t)std::min<uint64_t>(8192, ((uint64_t)b->n_sample * slices + kPolicyWaves - 1) / kPolicyWaves)};
+  if (b->n <= kAloneTokens && (uint64_t)b->n_sample * slices <= kAloneSlices) return Launch{slices, 16, 1};
+  return Launch{slices, 4, (uint32_t)std::min<uint64_t>(8192, ((uint64_t)b->n_sample * slices + 3) / 4)};
 }
+
+uint64_t work_of(const Launch &l) { return l.blocks > 1 ? (uint64_t)l.blocks * sizeof(Part) : 0; }
 
 }  // namespace
 
@@ -307,24 +315,30 @@ extern "C" int32_t vl_group_advantages(const vl_counts *counts, const float *ext
 extern "C" int32_t vl_policy_loss_work(const vl_policy_batch *batch, uint64_t *bytes) {
   if (!bytes) return VL_E_NULL;
   const int32_t rc = check_batch(batch);
-  if (rc == VL_OK) *bytes = (uint64_t)launch_of(batch).blocks * sizeof(Part);
+  if (rc == VL_OK) *bytes = work_of(launch_of(batch));
   return rc;
 }
 
 extern "C" int32_t vl_policy_loss(const vl_policy_batch *batch, float *grad, vl_policy_stats *stats, void *work, uint64_t work_bytes, vl_stream stream_) {
-  if (!grad || !stats || !work) return VL_E_NULL;
+  if (!grad || !stats) return VL_E_NULL;
   const int32_t rc = check_batch(batch);
   if (rc != VL_OK) return rc;
   const Launch launch = launch_of(batch);
-  if (work_bytes < launch.blocks * sizeof(Part) || (uintptr_t)work & 15 || (uintptr_t)grad & 3 || (uintptr_t)stats & 7) return VL_E_SHAPE;
+  if ((uintptr_t)grad & 3 || (uintptr_t)stats & 7) return VL_E_SHAPE;
+  if (const uint64_t need = work_of(launch)) {
+    if (!work) return VL_E_NULL;
+    if (work_bytes < need || (uintptr_t)work & 15) return VL_E_SHAPE;
+  }
   hipStream_t stream = (hipStream_t)stream_;
   const Batch b = {(const float VL_GLOBAL *)batch->logprob, (const float VL_GLOBAL *)batch->logprob_old, (const float VL_GLOBAL *)batch->logprob_ref,
                    (const uint64_t VL_GLOBAL *)batch->start, (const uint32_t VL_GLOBAL *)batch->len, (const float VL_GLOBAL *)batch->advantage,
                    (const float VL_GLOBAL *)batch->weight, (float VL_GLOBAL *)grad, batch->n, batch->n_sample, launch.slices,
                    batch->log_lo, batch->log_hi, batch->kl};
   Part VL_GLOBAL *parts = (Part VL_GLOBAL *)work;
-  (b.logprob_ref ? k_policy<true> : k_policy<false>)<<<launch.blocks, kPolicyThreads, 0, stream>>>(b, parts);
-  k_policy_join<<<1, kJoinThreads, 0, stream>>>(parts, launch.blocks, (vl_policy_stats VL_GLOBAL *)stats);
+  vl_policy_stats VL_GLOBAL *to = (vl_policy_stats VL_GLOBAL *)stats;
+  (b.logprob_ref ? launch.waves == 16 ? k_policy<true, 16> : k_policy<true, 4> : launch.waves == 16 ? k_policy<false, 16> : k_policy<false, 4>)
+      <<<launch.blocks, launch.waves * 64, 0, stream>>>(b, parts, to);
+  if (launch.blocks > 1) k_policy_join<<<1, kJoinThreads, 0, stream>>>(parts, launch.blocks, to);
   VL_HIP(hipGetLastError());
   return VL_OK;
 }

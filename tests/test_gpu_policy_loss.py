@@ -144,6 +144,15 @@ def test_many_ragged_samples(m):
     check_policy(make(start[order], length[order], int(length.sum()) + 1, m))
 
 
+@pytest.mark.parametrize("m,n_tok", [(1, 1), (1, 16384), (16, 1000), (17, 900), (32, 512), (33, 400), (1, 16385), (8, 2048), (4, 4096)])
+def test_small_batches(m, n_tok):
+    """around what one workgroup takes alone"""
+    for ref in (False, True):
+        b = make([k * n_tok for k in range(m)], [n_tok - (k % 3 if n_tok > 3 else 0) for k in range(m)], m * n_tok, m, ref)
+        check_policy(b)
+        check_policy(b, max_len=n_tok)
+
+
 def test_no_tokens_at_all():
     check_policy(make([0, 3], [0, 0], 5, 1))
 

@@ -115,8 +115,9 @@ def test_policy_refused():
         assert code(**{name: None}) == NULL, name
         assert code(**{name: P + 2}) == SHAPE, name
     assert code(start=P + 4) == SHAPE
-    assert code(grad=None) == NULL and code(stats=None) == NULL and code(work=None) == NULL
-    assert code(grad=P + 2) == SHAPE and code(stats=P + 4) == SHAPE and code(work=P + 8) == SHAPE and code(work_bytes=0) == SHAPE
+    many = dict(n=1 << 30, n_sample=1000)   # (few tokens need no work)
+    assert code(grad=None) == NULL and code(stats=None) == NULL and code(work=None, **many) == NULL
+    assert code(grad=P + 2) == SHAPE and code(stats=P + 4) == SHAPE and code(work=P + 8, **many) == SHAPE and code(work_bytes=0, **many) == SHAPE
     assert code(n=0) == SHAPE and code(n=1 << 60) == SHAPE and code(n_sample=0) == SHAPE and code(n_sample=1 << 31) == SHAPE
     for change in (dict(log_lo=0.3), dict(log_lo=float("nan")), dict(log_hi=float("nan")), dict(kl=float("nan")), dict(kl=float("inf")), dict(reserved0=1)):
         assert code(**change) == RANGE, change

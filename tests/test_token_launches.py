@@ -77,9 +77,11 @@ def test_the_others_launch_kernels_only(s):
         need = C.c_uint64()
         assert lib.vl_policy_loss_work(C.byref(batch), C.byref(need)) == 0
         s.launches.clear()
-        assert lib.vl_policy_loss(C.byref(batch), P, P, P, need.value, 0x77) == 0
-        first, second = s.launches
-        assert need.value == first[1][0] * 32 and 1 <= first[1][0] <= 8192 and second[1][0] == 1
-        s.launches.clear()
-        assert lib.vl_policy_loss(C.byref(batch), P, P, P, need.value - 1, 0x77) == -2 and not s.launches
+        assert lib.vl_policy_loss(C.byref(batch), P, P, P if need.value else None, need.value, 0x77) == 0
+        first, rest = s.launches[0], s.launches[1:]
+        blocks = first[1][0]
+        assert 1 <= blocks <= 8192 and need.value == (blocks * 32 if blocks > 1 else 0) and [x[1][0] for x in rest] == [1] * (blocks > 1)
+        if need.value:
+            s.launches.clear()
+            assert lib.vl_policy_loss(C.byref(batch), P, P, P, need.value - 1, 0x77) == -2 and not s.launches
     assert s.counts() == before
