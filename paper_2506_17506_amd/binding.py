@@ -403,7 +403,7 @@ class _Torch:
         self.words = (torch.int32, torch.uint32)
         self.longs = (torch.int64, torch.uint64)
         self.record = (torch.uint8, torch.int32, torch.uint32, torch.int64)
-        self.device = torch.cuda.current_device
+        self.device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.stream = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
         self.on, self.external = torch.cuda.stream, torch.cuda.ExternalStream
@@ -420,8 +420,9 @@ def _device_of(x, what):
     if _t is None:
         load()
         _t = _Torch()
-    if x.is_cuda and x.get_device() == _t.device():
-        return x.get_device()
+    device = x.get_device()   # (-1: the host)
+    if x.is_cuda and device == _t.device():
+        return device
     raise VlError(-7, what + _ELSEWHERE)
 
 
@@ -431,13 +432,11 @@ def _tensor(what, x, dtypes, shape, device, nullable=True):
         if nullable:
             return 0
         raise VlError(-1, what)
+    if x.get_device() == device and x.dtype in dtypes and (shape is None or x.shape == shape) and x.is_contiguous():
+        return x.data_ptr()
     if x.get_device() != device:
         raise VlError(-7, what + _ELSEWHERE)
-    if x.dtype not in dtypes:
-        raise VlError(-3, what)
-    if (shape is not None and x.shape != shape) or not x.is_contiguous():
-        raise VlError(-2, what)
-    return x.data_ptr()
+    raise VlError(-2 if x.dtype in dtypes else -3, what)
 
 
 def _row_pitch(what, x):
