@@ -106,7 +106,7 @@ struct BF16 {
   }
 };
 
-constexpr uint32_t kThreads = 256, kWaves = kThreads / 64, kQuarters = kThreads / 16;
+constexpr uint32_t kThreads = 256, kWaves = kThreads / 64;
 
 template <class T>
 __device__ inline u32x4 load_chunk(const uint8_t VL_GLOBAL *row, uint32_t c) {
@@ -393,29 +393,45 @@ __device__ inline void write_padding(const Scores &out, uint32_t r, uint32_t lan
   }
   if (lane < out.n_top) write_top<F32>(out, r, lane, 0, Final{0, 0, 0, 0, false});
 }
-// the given token's logit, -infinity if there is none
+// The given token's logit, and what says whether it counts: read at once and looked at last, so that nothing waits for them
+// one after the other.
 template <class T>
-__device__ inline float given_logit(const Rows &a, uint32_t r, int32_t token) {
-  if (!a.token || (uint32_t)token >= a.n_vocab) return kNoLogit;
-  if (a.mask && !((a.mask[(uint64_t)r * a.mask_ld + ((uint32_t)token >> 3)] >> (token & 7)) & 1)) return kNoLogit;
-  return T::wide(((const typename T::type VL_GLOBAL *)(a.logits + (uint64_t)r * a.ld))[token]);
+struct Given {
+  typename T::type x = (typename T::type)0;
+  uint32_t bits = 0;
+  __device__ inline float logit() const { return bits & 1u ? T::wide(x) : kNoLogit; }
+};
+template <class T>
+__device__ inline Given<T> given_logit(const Rows &a, uint32_t r, int32_t token) {
+  Given<T> g;
+  if (!a.token) return g;
+  const uint32_t t = min((uint32_t)token, a.n_vocab - 1);
+  g.x = ((const typename T::type VL_GLOBAL *)(a.logits + (uint64_t)r * a.ld))[t];
+  g.bits = a.mask ? (uint32_t)a.mask[(uint64_t)r * a.mask_ld + (t >> 3)] >> (t & 7) : 1u;
+  if (t != (uint32_t)token) g.bits = 0;
+  return g;
 }
 
-// Short rows of which no alternatives are asked for: 16 lanes per row, kChunks chunks per lane, so that a wavefront's
-// instructions for the reductions and the results serve four rows.  Four rows' loads are on their way at once.
-template <class T, uint32_t kChunks>
-__global__ __launch_bounds__(kThreads) void k_scores_quarter(Rows a, Scores out) {
-  const uint32_t lane = threadIdx.x & 15u;
-  for (uint32_t first = blockIdx.x * kQuarters; first < a.n_row; first += gridDim.x * kQuarters) {
-    const uint32_t r = first + (threadIdx.x >> 4);
+// Short rows of which no alternatives are asked for: 16 or 32 lanes per row, kChunks chunks per lane, so that a wavefront's
+// instructions for the reductions and the results serve four rows or two, whose loads are on their way at once.
+template <class T, uint32_t kTeam, uint32_t kChunks>
+__global__ __launch_bounds__(kThreads) void k_scores_few_lanes(Rows a, Scores out) {
+  constexpr uint32_t kTeams = kThreads / kTeam;
+  const uint32_t lane = threadIdx.x % kTeam;
+  auto fold = [](float x, auto f) {
+    x = quarter_fold(x, f);
+    return kTeam == 32 ? f(x, __shfl_xor(x, 16, 64)) : x;
+  };
+  for (uint32_t first = blockIdx.x * kTeams; first < a.n_row; first += gridDim.x * kTeams) {
+    const uint32_t r = first + threadIdx.x / kTeam;
     if (r >= a.n_row) break;
     const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
     const uint8_t VL_GLOBAL *mask = a.mask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
     const int32_t token = a.token ? a.token[r] : 0;
     float x[kChunks][T::kElems];
     uint32_t bits[kChunks];
-    load_row<T, 16, kChunks>(a, row, mask, lane, x, bits);
-    const float given = given_logit<T>(a, r, token);
+    load_row<T, kTeam, kChunks>(a, row, mask, lane, x, bits);
+    const Given<T> given = given_logit<T>(a, r, token);
 #pragma unroll
     for (uint32_t i = 0; i < kChunks; ++i)
       if (mask) keep_allowed<T>(x[i], bits[i]);
@@ -424,7 +440,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_quarter(Rows a, Scores out)
     for (uint32_t i = 0; i < kChunks; ++i)
 #pragma unroll
       for (uint32_t j = 0; j < T::kElems; ++j) m = fmaxf(m, x[i][j]);
-    Sums sums = {quarter_fold(m, [](float u, float v) { return fmaxf(u, v); }), 0.0f, 0.0f};
+    Sums sums = {fold(m, [](float u, float v) { return fmaxf(u, v); }), 0.0f, 0.0f};
     const float ref = ref_of(sums.m);
 #pragma unroll
     for (uint32_t i = 0; i < kChunks; ++i)
@@ -435,10 +451,10 @@ __global__ __launch_bounds__(kThreads) void k_scores_quarter(Rows a, Scores out)
         sums.y += e * fmaxf(z, kFar);
       }
     auto add = [](float u, float v) { return u + v; };
-    sums.s = quarter_fold(sums.s, add);
-    sums.y = quarter_fold(sums.y, add);
+    sums.s = fold(sums.s, add);
+    sums.y = fold(sums.y, add);
     if (token < 0) write_padding(out, r, lane);
-    else finish(a, out, r, sums, given, lane == 0);
+    else finish(a, out, r, sums, given.logit(), lane == 0);
   }
 }
 
@@ -458,7 +474,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
     float x[kChunks][T::kElems];
     uint32_t bits[kChunks];
     load_row<T, 64, kChunks>(a, row, mask, lane, x, bits);
-    const float given = given_logit<T>(a, r, token);
+    const Given<T> given = given_logit<T>(a, r, token);
 #pragma unroll
     for (uint32_t i = 0; i < kChunks; ++i)
       if (mask) keep_allowed<T>(x[i], bits[i]);
@@ -484,7 +500,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_short(Rows a, Scores out) {
       }
     sums.s = wave_sum(sums.s);
     if (out.entropy) sums.y = wave_sum(sums.y);
-    const Final f = finish(a, out, r, sums, given, lane == 0);
+    const Final f = finish(a, out, r, sums, given.logit(), lane == 0);
     if (out.n_top) {
       const uint32_t n = out.n_top;
       const uint64_t key = m == kNoLogit ? 0ull : key_of(ordered<T>(m), place);
@@ -608,7 +624,7 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
     }
     const uint32_t lead = lead_of<T>(row), n_full = (a.n_vocab + lead) / T::kElems, n_chunk = (a.n_vocab + lead + T::kElems - 1) / T::kElems;
     const uint32_t c1 = min(n_chunk, c0 + part_chunks), c1_full = min(n_full, c1);
-    const float given = parts ? kNoLogit : given_logit<T>(a, r, token);
+    const Given<T> given = parts ? Given<T>{} : given_logit<T>(a, r, token);
     Sums sums = {kNoLogit, 0.0f, 0.0f};
     uint32_t place = 0;        // the chunk that sums.m came from
     float second = kNoLogit;   // the largest logit of the other chunks
@@ -680,7 +696,7 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
     const float mine = sums.m;
     sums = join_sums(sh, sums, a.scale2);
     Final f = {};
-    if (!parts) f = finish(a, out, r, sums, given, threadIdx.x == 0);
+    if (!parts) f = finish(a, out, r, sums, given.logit(), threadIdx.x == 0);
     else if (threadIdx.x == 0) parts[(uint64_t)r * gridDim.x + blockIdx.x] = Part{sums.m, sums.s, sums.y, 0.0f};
     if (n_top) {
       const uint64_t key = mine == kNoLogit ? 0ull : key_of(ordered<T>(mine), place), least = least_of_interest<T>(sh, key, bits_for(n_chunk), n_top);
@@ -747,7 +763,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_join(Rows a, Scores out, ui
       write_padding(out, r, threadIdx.x);
       continue;
     }
-    const float given = given_logit<T>(a, r, token);
+    const Given<T> given = given_logit<T>(a, r, token);
     const uint64_t VL_GLOBAL *keys = part_keys + (uint64_t)r * n_part * n_top;
     uint64_t mine = 0;   // this thread's best of the parts' keys
     for (uint32_t i = threadIdx.x; i < n_part * n_top; i += kThreads) mine = keys[i] > mine ? keys[i] : mine;
@@ -757,7 +773,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_join(Rows a, Scores out, ui
       sums = Sums{p.x, p.y, p.z};
     }
     sums = join_sums(sh, sums, a.scale2);
-    const Final f = finish(a, out, r, sums, given, threadIdx.x == 0);
+    const Final f = finish(a, out, r, sums, given.logit(), threadIdx.x == 0);
     if (n_top) {
       // the keys that n of the threads' best reach
       const uint64_t least = least_of_interest<T>(sh, mine, bits_for(a.n_vocab), n_top);
@@ -996,8 +1012,10 @@ void launch_long(const Rows &a, const Scores &out, Split split, Part VL_GLOBAL *
 template <class T>
 void launch_scores(const Rows &a, const Scores &out, uint32_t n_chunk, Split split, void *work, hipStream_t stream) {
   if (n_chunk <= kShortChunks && !out.n_top) {
-    const uint32_t blocks = std::min((a.n_row + kQuarters - 1) / kQuarters, 1u << 20);
-    (n_chunk <= 16 ? k_scores_quarter<T, 1> : n_chunk <= 32 ? k_scores_quarter<T, 2> : n_chunk <= 64 ? k_scores_quarter<T, 4> : k_scores_quarter<T, 8>)
+    // 16 lanes per row while a lane has at most 4 chunks, then 32.  25,600 bf16 rows of 512: 9.6 us with 16 lanes, 10.1 with
+    // 32; rows of 1,024: 15.5 us with 16 lanes of 8 chunks, 12.5 with 32 of 4.
+    const uint32_t teams = kThreads / (n_chunk <= 64 ? 16 : 32), blocks = std::min((a.n_row + teams - 1) / teams, 1u << 20);
+    (n_chunk <= 16 ? k_scores_few_lanes<T, 16, 1> : n_chunk <= 32 ? k_scores_few_lanes<T, 16, 2> : n_chunk <= 64 ? k_scores_few_lanes<T, 16, 4> : k_scores_few_lanes<T, 32, 4>)
         <<<blocks, kThreads, 0, stream>>>(a, out);
     return;
   }
