@@ -135,6 +135,7 @@ struct Sample { uint64_t from, to; float a, w; };
 
 // A wavefront takes a slice of a sample at a time.  What bounds it: the arrays' bytes.  Whether d is past a bound is decided in 64
 // bits, where the difference of two numbers of 32 is exact (unless they are so far apart that no rounding matters), and every loss goes into a sum of 64 bits.
+// exp(d) and exp(q) are infinite above 88.7 in 32 bits: terms whose factor is 0 are left out, not multiplied by it.
 __device__ inline Part add_parts(Part p, const Part &q) { return Part{p.loss + q.loss, p.kl + q.kl, p.n_token + q.n_token, p.n_clipped + q.n_clipped}; }
 __device__ inline void write_stats(vl_policy_stats VL_GLOBAL *stats, const Part &p) {
   stats->loss = (float)p.loss;
@@ -167,17 +168,20 @@ __global__ __launch_bounds__(kWaves * 64) void k_policy(Batch b, Part VL_GLOBAL 
     auto token = [&](float lp, float old, float ref) {
       const double d = (double)lp - (double)old;
       const bool clip = d > hi || d < lo;
-      float l = -s.a * expf(clip ? bound : (float)d), g = clip ? 0.0f : l;
+      const float ratio = -s.a * expf(clip ? bound : (float)d);
+      float l = s.a == 0.0f ? 0.0f : ratio, g = clip ? 0.0f : l;
       if (kRef) {
         float gap, less_one;
         exp_gap(ref - lp, gap, less_one);
-        l += b.kl * gap;
-        g -= b.kl * less_one;
+        const float more = b.kl * gap, less = b.kl * less_one;
+        l += b.kl == 0.0f ? 0.0f : more;
+        g -= b.kl == 0.0f ? 0.0f : less;
         kl_sum += gap;
       }
       sum += l;
       n_clip += clip;
-      return s.w * g;
+      const float of = s.w * g;
+      return s.w == 0.0f ? 0.0f : of;
     };
     // steps start at multiples of kStep in the arrays, so that all but a sample's ends is read in whole lines
     for (uint64_t i = s.from / kStep * kStep; i < s.to; i += kStep) {
@@ -217,8 +221,10 @@ __global__ __launch_bounds__(kWaves * 64) void k_policy(Batch b, Part VL_GLOBAL 
           }
       }
     }
-    loss += (double)s.w * sum;
-    if (kRef) kls += (double)s.w * kl_sum;
+    if (s.w != 0.0f) {
+      loss += (double)s.w * sum;
+      if (kRef) kls += (double)s.w * kl_sum;
+    }
     tokens += s.to - s.from;   // (the same in all lanes)
     clips += n_clip;
   }

@@ -202,6 +202,29 @@ def test_extreme_log_probabilities():
     near(grad, g, np.where(np.isfinite(err), err, 0))
 
 
+@pytest.mark.parametrize("n_tok", [7, 700])   # (one launch, and parts that are joined)
+def test_factors_of_zero(n_tok):
+    # ratios and distances that 32 bits do not hold, in terms whose factor is 0: they add nothing
+    m = 100 if n_tok > 100 else 3
+    b = make([k * n_tok for k in range(m)], [n_tok] * m, m * n_tok, 8)
+    b["adv"][:3], b["weight"][:3] = (0.0, -2.0, 0.5), (0.25, 0.0, 0.125)
+    b["old"][:2 * n_tok] = b["lp"][:2 * n_tok] - 100
+    near_ref, b["ref"] = b["ref"], None
+    check_policy(b)
+    b["ref"] = near_ref
+    check_policy(b)
+    b["ref"][n_tok:2 * n_tok] += 120   # in the sample without weight
+    check_policy(b)
+    b["ref"][0] += 120
+    d = device(b)
+    grad, stats = torch.full_like(d["lp"], 77.0), torch.empty(24, dtype=torch.uint8, device="cuda")
+    call(d, grad, stats, kl=0.0)   # the distance is only reported
+    g, err, loss, loss_err = policy(b["lp"], b["old"], b["ref"], b["start"], b["length"], b["adv"], b["weight"], -0.25, 0.25, 0.0)[:4]
+    near(grad, g, err, "grad")
+    s = stats.cpu().numpy().view(vl.POLICY_STATS_DTYPE)[0]
+    assert abs(s["loss"] - loss) <= loss_err and s["kl"] == np.inf
+
+
 def test_gradient_against_differences():
     """of the loss in 64 bits, which check_policy holds the kernel's to: h = 2^-12 leaves h^2 / 6 times the third derivative"""
     b = make([0], [40], 40, 6)
