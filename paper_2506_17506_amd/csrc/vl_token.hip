@@ -650,14 +650,17 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
       }
       sums = rebase(sums, fmaxf(sums.m, m), a.scale2);
       const float ref = ref_of(sums.m);
+      float s = 0.0f, y = 0.0f;   // (of these chunks, so that long rows are not added up one by one)
 #pragma unroll
       for (uint32_t u = 0; u < kHere; ++u)
 #pragma unroll
         for (uint32_t j = 0; j < T::kElems; ++j) {
           const float z = (x[u][j] - ref) * a.scale2, e = __builtin_amdgcn_exp2f(z);
-          sums.s += e;
-          sums.y += e * fmaxf(z, kFar);
+          s += e;
+          y += e * fmaxf(z, kFar);
         }
+      sums.s += s;
+      sums.y += y;
     };
     for (uint32_t c = c0 + threadIdx.x; c - threadIdx.x < c1_full; c += kN * kTeam) {
       u32x4 w[kN];

@@ -259,6 +259,22 @@ def test_alternatives_that_stand_together(v, top):
             check_scores(out, Rows(y, None, top=top))
 
 
+@pytest.mark.parametrize("n,v", [(2048, 131072), (60, 1 << 20), (1, 1 << 24)])
+def test_many_equal_terms(n, v):
+    """a row's terms are not added up one by one: with 512 logits of x and the others 0, 64 lanes that take 32 at a time and 1,024
+    that take 16 make v / 2048 additions in a row at most, and some 50 for the batch and the joining"""
+    x = torch.zeros((n, v), dtype=F16, device="cuda")
+    x[:, :512] = 0.357
+    m = float(x[0, 0])
+    s = 512 + (v - 512) * np.exp(-m)
+    u = 2.0 ** -24
+    sum_err = u * (4 * m + 4 + v / 2048 + 50)
+    out = scores(x)
+    log_sum, share = np.log(s), (v - 512) * np.exp(-m) / s
+    near(out["stat"], np.tile([m, log_sum], (n, 1)), np.tile([0, sum_err + u * (log_sum + 2)], (n, 1)))
+    near(out["entropy"], np.full(n, log_sum + m * share), np.full(n, sum_err + m * (2 * sum_err + 12 * u) + 3 * u * log_sum))
+
+
 def test_outputs_that_are_not_asked_for():
     n, v = 6, 700
     x, t = bell(n, v, F16, 1), tokens(n, v, 2)
