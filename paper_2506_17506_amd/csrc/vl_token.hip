@@ -107,6 +107,7 @@ struct BF16 {
 };
 
 constexpr uint32_t kThreads = 256, kWaves = kThreads / 64;
+constexpr uint32_t kShortChunks = 128;   // 16-byte chunks of a row that a few lanes hold in registers
 
 template <class T>
 __device__ inline u32x4 load_chunk(const uint8_t VL_GLOBAL *row, uint32_t c) {
@@ -412,9 +413,10 @@ __device__ inline Given<T> given_logit(const Rows &a, uint32_t r, int32_t token)
   return g;
 }
 
-// Short rows of which no alternatives are asked for: 16 or 32 lanes per row, kChunks chunks per lane, so that a wavefront's
-// instructions for the reductions and the results serve four rows or two, whose loads are on their way at once.
-template <class T, uint32_t kTeam, uint32_t kChunks>
+// Short rows of which few alternatives are asked for, if any: 16 or 32 lanes per row, kChunks chunks per lane, so that a wavefront's
+// instructions for the reductions and the results serve four rows or two, whose loads are on their way at once.  Alternatives are
+// found one by one: the largest logit's first place, then the largest of the others.
+template <class T, uint32_t kTeam, uint32_t kChunks, bool kTop>
 __global__ __launch_bounds__(kThreads) void k_scores_few_lanes(Rows a, Scores out) {
   constexpr uint32_t kTeams = kThreads / kTeam;
   const uint32_t lane = threadIdx.x % kTeam;
@@ -453,8 +455,35 @@ __global__ __launch_bounds__(kThreads) void k_scores_few_lanes(Rows a, Scores ou
     auto add = [](float u, float v) { return u + v; };
     sums.s = fold(sums.s, add);
     sums.y = fold(sums.y, add);
-    if (token < 0) write_padding(out, r, lane);
-    else finish(a, out, r, sums, given.logit(), lane == 0);
+    if (token < 0) {
+      write_padding(out, r, lane);
+      continue;
+    }
+    const Final f = finish(a, out, r, sums, given.logit(), lane == 0);
+    if constexpr (kTop) {
+      m = sums.m;
+      for (uint32_t k = 0; ; ++k) {
+        uint32_t at = kShortChunks * T::kElems;   // of this lane's logits the first of this size; places counted from the lane's first
+#pragma unroll
+        for (int32_t i = kChunks - 1; i >= 0; --i)
+#pragma unroll
+          for (int32_t j = T::kElems - 1; j >= 0; --j) at = x[i][j] == m ? i * kTeam * T::kElems + j : at;
+        // (floats hold such places)
+        const uint32_t place = (uint32_t)fold((float)(at + lane * T::kElems), [](float u, float v) { return fminf(u, v); });
+        if (lane == 0) write_top<T>(out, r, k, m == kNoLogit ? 0ull : key_of(ordered<T>(m), place), f);
+        if (k + 1 == out.n_top) break;
+        m = kNoLogit;
+        at = place - lane * T::kElems;
+#pragma unroll
+        for (uint32_t i = 0; i < kChunks; ++i)
+#pragma unroll
+          for (uint32_t j = 0; j < T::kElems; ++j) {
+            if (at == i * kTeam * T::kElems + j) x[i][j] = kNoLogit;
+            m = fmaxf(m, x[i][j]);
+          }
+        m = fold(m, [](float u, float v) { return fmaxf(u, v); });
+      }
+    }
   }
 }
 
@@ -928,7 +957,6 @@ __global__ __launch_bounds__(kThreads) void k_grad_long(Rows a, Grad b, uint32_t
 // ---- host
 
 constexpr uint32_t kMostRows = 0x7FFFFFFFu;
-constexpr uint32_t kShortChunks = 128;       // 16-byte chunks of a row that a few lanes hold in registers
 constexpr uint32_t kShortGradChunks = 256;
 constexpr uint32_t kMostGridY = 65535;
 
@@ -1014,12 +1042,23 @@ void launch_long(const Rows &a, const Scores &out, Split split, Part VL_GLOBAL *
 }
 template <class T>
 void launch_scores(const Rows &a, const Scores &out, uint32_t n_chunk, Split split, void *work, hipStream_t stream) {
-  if (n_chunk <= kShortChunks && !out.n_top) {
+  // Short rows, few lanes each: no alternatives, or few enough.  25,600 bf16 rows, us this way / with a wavefront each and its search: of 512,
+  // one alternative 10.3 / 16.8, two 12.7 / 17.2, four 17.6 / 17.8; of 128, one 4.8 / 15.0, eight 12.1 / 17.6; in 32 bits of
+  // 256, four 12.8 / 15.9, eight 19.0 / 16.7.  An alternative more takes 0.35 to 0.85 us even of few rows, where the search's take
+  // 0.05 (one alternative of 500 rows of 512 3.95 / 3.92, two 4.8 / 4.0; of 4,000 rows two 4.86 / 4.86; four of rows of 256, 4,000 of
+  // them 5.0 / 5.0, 8,000 5.6 / 7.2; eight of rows of 128, 4,000 of them 5.6 / 5.3, 8,000 6.1 / 7.6).
+  const uint32_t held = (n_chunk <= 16 ? 1u : n_chunk <= 32 ? 2u : 4u) * T::kElems;   // logits of a lane
+  if (n_chunk <= kShortChunks && (out.n_top <= 1 || (out.n_top * held <= 64 && a.n_row >= 512 * (out.n_top + 5)))) {
     // 16 lanes per row while a lane has at most 4 chunks, then 32.  25,600 bf16 rows of 512: 9.6 us with 16 lanes, 10.1 with
     // 32; rows of 1,024: 15.5 us with 16 lanes of 8 chunks, 12.5 with 32 of 4.
     const uint32_t teams = kThreads / (n_chunk <= 64 ? 16 : 32), blocks = std::min((a.n_row + teams - 1) / teams, 1u << 20);
-    (n_chunk <= 16 ? k_scores_few_lanes<T, 16, 1> : n_chunk <= 32 ? k_scores_few_lanes<T, 16, 2> : n_chunk <= 64 ? k_scores_few_lanes<T, 16, 4> : k_scores_few_lanes<T, 32, 4>)
-        <<<blocks, kThreads, 0, stream>>>(a, out);
+    auto launch = [&](auto top) {
+      constexpr bool kTop = decltype(top)::value;
+      (n_chunk <= 16 ? k_scores_few_lanes<T, 16, 1, kTop> : n_chunk <= 32 ? k_scores_few_lanes<T, 16, 2, kTop> : n_chunk <= 64 ? k_scores_few_lanes<T, 16, 4, kTop> : k_scores_few_lanes<T, 32, 4, kTop>)
+          <<<blocks, kThreads, 0, stream>>>(a, out);
+    };
+    if (out.n_top) launch(std::true_type{});
+    else launch(std::false_type{});
     return;
   }
   if (n_chunk <= kShortChunks) {

@@ -238,6 +238,31 @@ def test_alternatives_among_equal_logits(n, v, top):
         check_all(y, None, top=top, what=f"distance {step}")
 
 
+@pytest.mark.parametrize("v,dtype,top", [(1, BF16, 8), (9, F16, 8), (127, BF16, 3), (128, BF16, 8), (250, F16, 4), (512, BF16, 2), (1023, F16, 2), (1024, BF16, 1),
+                                         (64, F32, 16), (128, F32, 8), (129, F32, 4), (256, F32, 4), (500, F32, 1)])
+def test_few_alternatives_of_many_short_rows(v, dtype, top):
+    rows = odd_rows(v, dtype)
+    x = torch.stack([r[0] for r in rows]).to(dtype).cuda()
+    n = 2048 * top + 13   # (teams of lanes without a row at the end)
+    which = torch.arange(n) % len(rows)
+    bits = np.stack([r[2] for r in rows])
+    t = torch.tensor([r[1] for r in rows], dtype=torch.int32)[which].cuda()
+    for mask in (None, words_of(bits)[which].cuda()):
+        few = scores(x, None, None if mask is None else words_of(bits).cuda(), top=top)
+        check_scores(few, Rows(x, None, None if mask is None else words_of(bits).cuda(), top=top), "few rows")
+        out = scores(x[which.cuda()], t, mask, top=top)
+        there = t >= 0
+        for k in ("top_token", "top_logprob", "stat", "entropy"):   # few rows take another way
+            a, b = out[k][there].float(), few[k][which.cuda()][there].float()
+            assert torch.allclose(a, b, rtol=2.0 ** -18, atol=2.0 ** -18, equal_nan=True) and (k != "top_token" or (a == b).all()), k
+        assert (out["top_token"][~there] == -1).all()
+    y = bell(n, v, dtype, top)
+    y = (y.float() * 4).round().to(dtype)   # many are equal
+    want = y.float().sort(dim=1, descending=True, stable=True).indices[:, :top].int()
+    got = scores(y, None, top=top)["top_token"]
+    assert (got[:, :min(top, v)] == want).all() and (got[:, v:] == -1).all()
+
+
 @pytest.mark.parametrize("v", [512, 4096, 32768, 131072, 1 << 20])
 @pytest.mark.parametrize("top", [1, 8, 20, 32])
 def test_alternatives_that_stand_together(v, top):
