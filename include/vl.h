@@ -360,7 +360,7 @@ int32_t vl_free_bases_multi(const vl_mask_query *queries, uint32_t n, uint32_t *
  * and no alternatives.  If an allowed logit is NaN or +infinity every number of the row is NaN and its alternatives'
  * tokens are -1.  Sums and statistics are held in 32 bits whatever the logits' type.
  * Results do not depend on what else runs, and a row's not on the other rows; the number of rows
- * decides how a row's sum is split, so its last bits may differ between calls of other sizes. */
+ * and a row's alignment decide how its sum is split, so its last bits may differ between calls of other sizes or places. */
 enum { VL_F32 = 0, VL_F16 = 1, VL_BF16 = 2 };
 #define VL_MAX_VOCAB (1u << 24)
 #define VL_MAX_TOP 32u

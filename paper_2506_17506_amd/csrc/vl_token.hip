@@ -569,6 +569,7 @@ typedef float Part __attribute__((ext_vector_type(4)));
 template <uint32_t kTeam>
 struct Shared {
   Sums sums[kTeam / 64];
+  float token[kTeam / 64];
   Room<kTeam> room;
   uint64_t key[kTeam < 64 ? 64 : kTeam];
   uint64_t list[kTeam / 64 * VL_MAX_TOP];   // (a multiple of four long)
@@ -615,34 +616,47 @@ __device__ inline uint64_t least_of_interest(Shared<kTeam> &sh, uint64_t mine, u
   return sh.least;
 }
 
-template <uint32_t kTeam>
-__device__ inline Sums join_sums(Shared<kTeam> &sh, Sums mine, float scale2) {
+// The sums of all of a workgroup's threads.  With kOne `token`, of each thread the first token of its largest logit, becomes the first of
+// the largest of all.  (Tokens are below 2^24: floats hold them.)
+constexpr float kBehind = 0x1p24f;
+template <uint32_t kTeam, bool kOne = false>
+__device__ inline Sums join_sums(Shared<kTeam> &sh, Sums mine, float scale2, float *token = nullptr) {
   auto add = [](float u, float v) { return u + v; };
-  mine = rebase(mine, wave_max(mine.m), scale2);
+  auto lower = [](float u, float v) { return fminf(u, v); };
+  const float most = wave_max(mine.m);
+  if (kOne) *token = wave_fold(mine.m == most ? *token : kBehind, kBehind, lower);
+  mine = rebase(mine, most, scale2);
   mine.s = wave_sum(mine.s);
   mine.y = wave_sum(mine.y);
   if constexpr (kTeam == 64) return mine;
-  if ((threadIdx.x & 63u) == 0) sh.sums[threadIdx.x >> 6] = mine;
+  if ((threadIdx.x & 63u) == 0) {
+    sh.sums[threadIdx.x >> 6] = mine;
+    if (kOne) sh.token[threadIdx.x >> 6] = *token;
+  }
   __syncthreads();
   const uint32_t w = threadIdx.x & 15u;   // (16 wavefronts at most)
   mine = w < kTeam / 64 ? sh.sums[w] : Sums{kNoLogit, 0.0f, 0.0f};
-  mine = rebase(mine, quarter_fold(mine.m, [](float u, float v) { return fmaxf(u, v); }), scale2);
+  const float best = quarter_fold(mine.m, [](float u, float v) { return fmaxf(u, v); });
+  if (kOne) *token = quarter_fold(w < kTeam / 64 && mine.m == best ? sh.token[w] : kBehind, lower);
+  mine = rebase(mine, best, scale2);
   mine.s = quarter_fold(mine.s, add);
   mine.y = quarter_fold(mine.y, add);
   return mine;
 }
 
 
-// what is asked for: alternatives too or sums alone; and whether nothing of the logits is kept in the caches
-enum Kind { kWithTop, kWithTopOnce, kSums, kSumsOnce };
+// what is asked for: alternatives too, just one, or sums alone; and whether nothing of the logits is kept in the caches
+enum Kind { kWithTop, kWithTopOnce, kWithOne, kWithOneOnce, kSums, kSumsOnce };
 constexpr uint32_t kFewChunks = 4;
 
 // Long rows: a workgroup of kTeam threads per row or part of a row.  Thread t takes the part's chunks t, t + kTeam, t + 2 kTeam, ...
-// kN chunks of a lane are on their way at once.
+// kN chunks of a lane are on their way at once.  If one alternative is asked for, a lane keeps its best chunk in registers.
 template <class T, uint32_t kTeam, uint32_t kN, bool kMask, Kind kKind>
 __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_scores_long(Rows a, Scores out, uint32_t part_chunks, Part VL_GLOBAL *parts, uint64_t VL_GLOBAL *part_keys) {
   __shared__ Shared<kTeam> sh;
-  const uint32_t c0 = blockIdx.x * part_chunks, n_top = kKind <= kWithTopOnce ? out.n_top : 0;
+  constexpr bool kTop = kKind == kWithTop || kKind == kWithTopOnce, kOne = kKind == kWithOne || kKind == kWithOneOnce;
+  constexpr bool kOnce = kKind == kWithTopOnce || kKind == kWithOneOnce || kKind == kSumsOnce;
+  const uint32_t c0 = blockIdx.x * part_chunks, n_top = kTop ? out.n_top : 0;
   for (uint32_t r = blockIdx.y; r < a.n_row; r += gridDim.y) {
     const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
     const uint8_t VL_GLOBAL *mask = kMask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
@@ -657,8 +671,10 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
     Sums sums = {kNoLogit, 0.0f, 0.0f};
     uint32_t place = 0;        // the chunk that sums.m came from
     float second = kNoLogit;   // the largest logit of the other chunks
+    u32x4 kept = {T::kNone, T::kNone, T::kNone, T::kNone};   // that chunk
+    uint32_t kept_bits = 0;
     // kHere chunks of this lane from c on, kTeam apart
-    auto add = [&](auto n_of, const float (*x)[T::kElems], uint32_t c) {
+    auto add = [&](auto n_of, const float (*x)[T::kElems], uint32_t c, const u32x4 *w, const uint32_t *bits) {
       constexpr uint32_t kHere = decltype(n_of)::value;
       float b[kHere], m = kNoLogit;
 #pragma unroll
@@ -668,12 +684,17 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
         for (uint32_t j = 1; j < T::kElems; ++j) b[u] = fmaxf(b[u], x[u][j]);
         m = fmaxf(m, b[u]);
       }
-      if (kKind <= kWithTopOnce) {
+      if (kTop || kOne) {
         float best = sums.m;
 #pragma unroll
         for (uint32_t u = 0; u < kHere; ++u) {
-          second = __builtin_amdgcn_fmed3f(best, second, b[u]);   // (second <= best)
+          if (kTop) second = __builtin_amdgcn_fmed3f(best, second, b[u]);   // (second <= best)
           place = b[u] > best ? c + u * kTeam : place;
+          if (kOne) {
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) kept[j] = b[u] > best ? w[u][j] : kept[j];
+            if (kMask) kept_bits = b[u] > best ? bits[u] : kept_bits;
+          }
           best = fmaxf(best, b[u]);
         }
       }
@@ -696,7 +717,7 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
       uint32_t bits[kN];
       if (c - threadIdx.x + kN * kTeam <= c1_full) {
 #pragma unroll
-        for (uint32_t u = 0; u < kN; ++u) w[u] = kKind == kSumsOnce || kKind == kWithTopOnce ? load_once<T>(row, lead, c + u * kTeam) : load_even<T>(row, lead, c + u * kTeam);
+        for (uint32_t u = 0; u < kN; ++u) w[u] = kOnce ? load_once<T>(row, lead, c + u * kTeam) : load_even<T>(row, lead, c + u * kTeam);
         if (kMask) {
 #pragma unroll
           for (uint32_t u = 0; u < kN; ++u) bits[u] = mask_bits<T>(mask, lead, c + u * kTeam);
@@ -718,18 +739,36 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
         if (kMask) keep_allowed<T>(x[u], bits[u]);
       }
       if (lead > c) x[0][0] = kNoLogit;
-      add(std::integral_constant<uint32_t, kN>{}, x, c);
+      add(std::integral_constant<uint32_t, kN>{}, x, c, w, bits);
     }
     if (n_full < c1 && threadIdx.x == (n_full - c0) % kTeam) {   // the chunk that the row's end cuts
       float x[1][T::kElems];
       load_any<T>(a, row, mask, lead, n_full, x[0]);
-      add(std::integral_constant<uint32_t, 1>{}, x, n_full);
+      const u32x4 w = kOne ? T::pack(x[0]) : u32x4{};   // (as it was: these are the type's own values)
+      const uint32_t bits = ~0u;
+      add(std::integral_constant<uint32_t, 1>{}, x, n_full, &w, &bits);
     }
     const float mine = sums.m;
-    sums = join_sums(sh, sums, a.scale2);
+    float first = kBehind;
+    if constexpr (kOne) {
+      float x[T::kElems];
+      T::unpack(kept, x);
+      if (kMask) keep_allowed<T>(x, kept_bits);
+      if (lead > place) x[0] = kNoLogit;
+      uint32_t at = 0;
+#pragma unroll
+      for (int32_t j = T::kElems - 1; j >= 0; --j) at = x[j] == mine ? j : at;
+      first = (float)(int32_t)(place * T::kElems - lead + at);
+    }
+    sums = join_sums<kTeam, kOne>(sh, sums, a.scale2, &first);
     Final f = {};
     if (!parts) f = finish(a, out, r, sums, given.logit(), threadIdx.x == 0);
     else if (threadIdx.x == 0) parts[(uint64_t)r * gridDim.x + blockIdx.x] = Part{sums.m, sums.s, sums.y, 0.0f};
+    if (kOne && threadIdx.x == 0) {
+      const uint64_t best = sums.m == kNoLogit ? 0ull : key_of(ordered<T>(sums.m), (uint32_t)first);
+      if (!parts) write_top<T>(out, r, 0, best, f);
+      else part_keys[(uint64_t)r * gridDim.x + blockIdx.x] = best;
+    }
     if (n_top) {
       const uint64_t key = mine == kNoLogit ? 0ull : key_of(ordered<T>(mine), place), least = least_of_interest<T>(sh, key, bits_for(n_chunk), n_top);
       const bool hot = key >= least;
@@ -799,14 +838,17 @@ __global__ __launch_bounds__(kThreads) void k_scores_join(Rows a, Scores out, ui
     const uint64_t VL_GLOBAL *keys = part_keys + (uint64_t)r * n_part * n_top;
     uint64_t mine = 0;   // this thread's best of the parts' keys
     for (uint32_t i = threadIdx.x; i < n_part * n_top; i += kThreads) mine = keys[i] > mine ? keys[i] : mine;
+    float first = (float)~(uint32_t)mine;   // (if there is one key per part)
     Sums sums = {kNoLogit, 0.0f, 0.0f};
     if (threadIdx.x < n_part) {   // (never more than there are threads)
       const Part p = parts[(uint64_t)r * n_part + threadIdx.x];
       sums = Sums{p.x, p.y, p.z};
     }
-    sums = join_sums(sh, sums, a.scale2);
+    sums = join_sums<kThreads, true>(sh, sums, a.scale2, &first);
     const Final f = finish(a, out, r, sums, given.logit(), threadIdx.x == 0);
-    if (n_top) {
+    if (n_top == 1) {
+      if (threadIdx.x == 0) write_top<T>(out, r, 0, sums.m == kNoLogit ? 0ull : key_of(ordered<T>(sums.m), (uint32_t)first), f);
+    } else if (n_top) {
       // the keys that n of the threads' best reach
       const uint64_t least = least_of_interest<T>(sh, mine, bits_for(a.n_vocab), n_top);
       if (mine >= least) {
@@ -1028,17 +1070,19 @@ void launch_long(const Rows &a, const Scores &out, Split split, Part VL_GLOBAL *
   // Logits beyond what the Infinity Cache holds (256 MB) are not kept in the caches: 1,500 rows of 131,072 77 -> 69 us,
   // 8,000 of 20,000 65 -> 56, with five alternatives 4,096 of 50,001 85 -> 82; but 64 MB that the program before has just written
   // 17.7 -> 19.9.
+  auto launch = [&](auto with_top, auto with_one, auto sums) {
+    constexpr Kind kTop = decltype(with_top)::value, kOne = decltype(with_one)::value, kNone = decltype(sums)::value;
+    (a.mask ? out.n_top > 1 ? k_scores_long<T, kTeam, kN, true, kTop> : out.n_top ? k_scores_long<T, kTeam, kN, true, kOne> : k_scores_long<T, kTeam, kN, true, kNone>
+            : out.n_top > 1 ? k_scores_long<T, kTeam, kN, false, kTop> : out.n_top ? k_scores_long<T, kTeam, kN, false, kOne> : k_scores_long<T, kTeam, kN, false, kNone>)
+        <<<grid, kTeam, 0, stream>>>(a, out, split.chunks, parts, keys);
+  };
   if constexpr (kTeam != 1024 || kN != 4) {   // (fewer than 128 rows are never that much)
     if ((uint64_t)a.n_row * a.n_vocab * sizeof(typename T::type) > (256ull << 20)) {
-      (a.mask ? out.n_top ? k_scores_long<T, kTeam, kN, true, kWithTopOnce> : k_scores_long<T, kTeam, kN, true, kSumsOnce>
-              : out.n_top ? k_scores_long<T, kTeam, kN, false, kWithTopOnce> : k_scores_long<T, kTeam, kN, false, kSumsOnce>)
-          <<<grid, kTeam, 0, stream>>>(a, out, split.chunks, parts, keys);
+      launch(std::integral_constant<Kind, kWithTopOnce>{}, std::integral_constant<Kind, kWithOneOnce>{}, std::integral_constant<Kind, kSumsOnce>{});
       return;
     }
   }
-  (a.mask ? out.n_top ? k_scores_long<T, kTeam, kN, true, kWithTop> : k_scores_long<T, kTeam, kN, true, kSums>
-          : out.n_top ? k_scores_long<T, kTeam, kN, false, kWithTop> : k_scores_long<T, kTeam, kN, false, kSums>)
-      <<<grid, kTeam, 0, stream>>>(a, out, split.chunks, parts, keys);
+  launch(std::integral_constant<Kind, kWithTop>{}, std::integral_constant<Kind, kWithOne>{}, std::integral_constant<Kind, kSums>{});
 }
 template <class T>
 void launch_scores(const Rows &a, const Scores &out, uint32_t n_chunk, Split split, void *work, hipStream_t stream) {

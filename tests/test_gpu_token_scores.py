@@ -263,6 +263,28 @@ def test_few_alternatives_of_many_short_rows(v, dtype, top):
     assert (got[:, :min(top, v)] == want).all() and (got[:, v:] == -1).all()
 
 
+@pytest.mark.parametrize("v,dtype,n", [(1041, BF16, 27), (2500, F32, 300), (1100, F16, 1200), (1033, BF16, 2500), (515, F32, 2100), (20011, BF16, 130), (70001, F16, 20), (33001, F32, 27),
+                                       (131073, BF16, 2)])
+@pytest.mark.parametrize("first", [0, 1])
+def test_one_alternative_of_long_rows(v, dtype, n, first):
+    """odd values and equal logits, in rows that start at even and odd places"""
+    rows = odd_rows(v, dtype)[-n:]
+    which = torch.arange(n) % len(rows)
+    small = torch.stack([r[0] for r in rows]).to(dtype)
+    x = torch.full((n, v + first + 2), float("nan"), dtype=dtype, device="cuda")[:, first:first + v]
+    x.copy_(small[which])
+    t = torch.tensor([r[1] for r in rows], dtype=torch.int32)[which].cuda()
+    bits = words_of(np.stack([r[2] for r in rows]))
+    for mask in (None, bits):
+        want = Rows(small, t[:len(rows)], mask, top=1)
+        out = scores(x, t, None if mask is None else mask[which].cuda(), top=1)
+        for at in range(0, n, len(rows)):   # (rows at odd and even places are summed in chunks of their own: none equals another in its last bits)
+            some = min(len(rows), n - at)
+            if some < len(rows):
+                want = Rows(small[:some], t[:some], None if mask is None else mask[:some], top=1)
+            check_scores({k: o[at:at + some] for k, o in out.items()}, want, f"rows from {at} on")
+
+
 @pytest.mark.parametrize("v", [512, 4096, 32768, 131072, 1 << 20])
 @pytest.mark.parametrize("top", [1, 8, 20, 32])
 def test_alternatives_that_stand_together(v, top):
