@@ -1035,24 +1035,26 @@ Rows device_rows(const vl_token_rows *a) {
               (const int32_t VL_CONSTANT *)a->token, a->n_row, a->n_vocab, a->scale, (float)((double)a->scale * 1.4426950408889634)};
 }
 
-// How many threads a workgroup has, how many workgroups share a row, and how many chunks each takes.  A wavefront per row where there are
-// rows for all wavefronts, if no alternatives are asked for or the row is short (they are found in a share of the row that
-// falls with the threads); more threads per row the fewer rows there are; and parts, which a second launch joins, where few rows
-// are too long for one workgroup.  Measured, us (this choice / the other):
-//   3,000 x 5,000, no alternatives: 64 threads 10.5 / 256 13.2;      4,096 x 20,000, twenty: 64 46 / 256 48
+// How many threads a workgroup has, how many workgroups share a row, and how many chunks each takes.  A wavefront per row where it is short
+// or there are rows for all wavefronts (with alternatives, which are found in a share of the row that falls with the threads, not if
+// it is very long); more threads the longer the row and the fewer rows there are; and parts, which a second launch joins, where few
+// rows are too long for one workgroup.  Measured, us (this choice / the others), bf16 logits:
+//   1,000 x 2,000: 64 threads 3.9 / 256 5.2, 1,024 8.8; five alternatives 6.1 / 8.4, 16.3
+//   600 x 4,000: 64 4.5 / 256 4.8, 1,024 7.3;                          1 x 4,000: 256 3.4 / 64 3.8
+//   3,000 x 5,000: 64 10.5 / 256 13.2;                                 4,096 x 20,000, twenty: 64 46 / 256 48
 //   (4,096 x 50,001 in 32 bits, five, 12,501 chunks: 256 73.7 / 64 77.4)
-//   500 x 32,000 in 32 bits: 1,024 in 1 part 17.7 / 256 in 4 24.0;   300 x 50,001: 1,024 17.8 / 256 in 5 20.7
-//   1 x 32,000: 1,024 in 1 part 9.4 / 256 in 7 11.6;                 1 x 131,072: 256 in 21 parts 10.2 / in 32 10.6, 1,024 in 1 15.3
-//   1 x 5,000: 256 6.9 / 1,024 9.3;                                  100 x 131,072: 1,024 in 1 part 16.2 / in 5 17.6
+//   1,000 x 16,000, five: 256 12.8 / 64 15.0, 1,024 17.9;              1 x 16,000: 256 4.2 / 1,024 4.6
+//   500 x 32,000 in 32 bits, one: 256 14.8 / 1,024 15.9;               500 x 100,000: 1,024 24.2 / 256 26.9
+//   150 x 32,000: 1,024 5.9 / 256 7.2, in 3 parts 9.2;                 1 x 32,000: 1,024 4.7 / 256 5.6
+//   1 x 131,072, twenty: 256 in 21 parts 10.2 / in 32 10.6, 1,024 15.3; 60: 256 in 21 parts 15.0 / 1,024 16.5, 128: 1,024 16.7 / in 16 parts 19.6
 struct Split { uint32_t team, parts, chunks; bool few; };   // few: a compute unit has one workgroup at most, which may use twice the registers
 Split split_of(const vl_token_rows *a, uint32_t n_top, bool lead) {
   const uint32_t n = chunks_of(a, lead), rows = a->n_row;
-  const bool few = rows < 128;
+  const bool few = rows <= 256;
   uint32_t team = 1024, parts = 1;
-  if (rows >= 2048 && (n_top == 0 || n <= 8192)) team = 64;
-  else if (rows >= 1024 || (few && n <= 1024)) team = 256;
-  else if (!few) parts = std::max(1u, std::min(512 / rows, n / 1024));
-  else if (rows < 48 && n > 8192) { team = 256; parts = std::min({2048 / rows, n / 768, 256u}); }
+  if (n <= 256 || (n <= 512 && rows >= 600) || (rows >= 2048 && (n_top == 0 || n <= 8192))) team = 64;
+  else if (n <= 2048 || rows > 512 || (!few && n <= 8192)) team = 256;
+  else if (rows < 96 && n > 8192) { team = 256; parts = std::min({2048 / rows, n / 768, 256u}); }
   if (parts == 1) return Split{team, 1, n, few};
   const uint32_t chunks = ((n + parts - 1) / parts + team - 1) / team * team;
   return Split{team, (n + chunks - 1) / chunks, chunks, few};
@@ -1076,7 +1078,7 @@ void launch_long(const Rows &a, const Scores &out, Split split, Part VL_GLOBAL *
             : out.n_top > 1 ? k_scores_long<T, kTeam, kN, false, kTop> : out.n_top ? k_scores_long<T, kTeam, kN, false, kOne> : k_scores_long<T, kTeam, kN, false, kNone>)
         <<<grid, kTeam, 0, stream>>>(a, out, split.chunks, parts, keys);
   };
-  if constexpr (kTeam != 1024 || kN != 4) {   // (fewer than 128 rows are never that much)
+  if constexpr (kTeam != 1024 || kN != 4) {   // (256 rows or fewer are seldom that much)
     if ((uint64_t)a.n_row * a.n_vocab * sizeof(typename T::type) > (256ull << 20)) {
       launch(std::integral_constant<Kind, kWithTopOnce>{}, std::integral_constant<Kind, kWithOneOnce>{}, std::integral_constant<Kind, kSumsOnce>{});
       return;
