@@ -113,6 +113,10 @@ template <class T>
 __device__ inline u32x4 load_chunk(const uint8_t VL_GLOBAL *row, uint32_t c) {
   return *(const typename T::chunk VL_GLOBAL *)(row + (uint64_t)c * 16);
 }
+template <class T>
+__device__ inline u32x4 load_once(const uint8_t VL_GLOBAL *row, uint32_t c) {   // nothing of it is kept in the caches
+  return __builtin_nontemporal_load((const typename T::chunk VL_GLOBAL *)(row + (uint64_t)c * 16));
+}
 // Long rows of 16 bits a logit are taken from the multiple of 4 bytes at or below their start, `lead` (0 or 1) logits early,
 // since loads from odd places cost: 4,096 rows of 50,001 logits 91 us, of 50,000 78.  Chunk c then holds tokens
 // c * 8 - lead and up; what stands before the row does not count.  (It lies in the word that holds the row's first logit.)
@@ -917,7 +921,8 @@ __device__ inline void grad_chunk(const Rows &a, const GradRow &g, uint32_t c, f
       x[j] = as_float(as_word(x[j]) & (uint32_t)((int32_t)(bits << (31 - j)) >> 31));
   }
 }
-// (not kept in the caches of a die, which others could not use: 25,600 rows of 1,024 25.8 -> 22.4 us)
+// (not kept in the caches of a die, which others could not use: 25,600 rows of 1,024 25.8 -> 22.4 us, 400 of 80,000 28.1 -> 22.3, 8,192 of
+// 131,072 745 -> 733; but 100 of 2,900 3.7 -> 4.0)
 template <class T>
 __device__ inline void store_any(const Rows &a, uint8_t VL_GLOBAL *to, uint32_t c, const float *x) {
   const uint32_t from = c * T::kElems;
@@ -956,9 +961,10 @@ __global__ __launch_bounds__(kThreads) void k_grad_short(Rows a, Grad b) {
   }
 }
 
-constexpr uint32_t kBatch = 4;   // chunks of a lane on their way at once
-template <class T, bool kMask>
-__global__ __launch_bounds__(kThreads) void k_grad_long(Rows a, Grad b, uint32_t piece_chunks) {
+// Long rows: a workgroup per piece of a row, of kBatch chunks for each thread, all on their way at once.  kOnce: the logits are not kept in the caches.
+template <class T, bool kMask, bool kOnce, uint32_t kBatch>
+__global__ __launch_bounds__(kThreads) void k_grad_long(Rows a, Grad b) {
+  constexpr uint32_t piece_chunks = kBatch * kThreads;
   const uint32_t n_full = a.n_vocab / T::kElems, n_chunk = (a.n_vocab + T::kElems - 1) / T::kElems;
   const uint32_t c0 = blockIdx.x * piece_chunks, c1 = min(n_chunk, c0 + piece_chunks), c1_full = min(n_full, c1);
   for (uint32_t r = blockIdx.y; r < a.n_row; r += gridDim.y) {
@@ -972,26 +978,32 @@ __global__ __launch_bounds__(kThreads) void k_grad_long(Rows a, Grad b, uint32_t
       for (; c < c1; c += kThreads) store_any<T>(a, to, c, x);
       continue;
     }
-    for (; c - threadIdx.x + kBatch * kThreads <= c1_full; c += kBatch * kThreads) {
-      u32x4 w[kBatch];
-      uint32_t bits[kBatch];
+    u32x4 w[kBatch];
+    uint32_t bits[kBatch];
+    const bool all = c0 + piece_chunks <= c1_full;
 #pragma unroll
-      for (uint32_t u = 0; u < kBatch; ++u) w[u] = load_chunk<T>(row, c + u * kThreads);
-#pragma unroll
-      for (uint32_t u = 0; u < kBatch; ++u) bits[u] = kMask ? mask_bits<T>(mask, c + u * kThreads) : 0u;
-#pragma unroll
-      for (uint32_t u = 0; u < kBatch; ++u) {
-        float x[T::kElems];
-        T::unpack(w[u], x);
-        grad_chunk<T>(a, g, c + u * kThreads, x, bits[u], kMask);
-        *(typename T::chunk VL_GLOBAL *)(to + (uint64_t)(c + u * kThreads) * 16) = T::pack(x);
-      }
+    for (uint32_t u = 0; u < kBatch; ++u) {
+      w[u] = u32x4{};
+      if (all || c + u * kThreads < c1_full) w[u] = kOnce ? load_once<T>(row, c + u * kThreads) : load_chunk<T>(row, c + u * kThreads);
     }
-    for (; c < c1; c += kThreads) {
+#pragma unroll
+    for (uint32_t u = 0; u < kBatch; ++u) {
+      bits[u] = 0;
+      if (kMask && (all || c + u * kThreads < c1_full)) bits[u] = mask_bits<T>(mask, c + u * kThreads);
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < kBatch; ++u) {
+      if (!all && c + u * kThreads >= c1_full) break;
       float x[T::kElems];
-      load_any<T>(a, row, nullptr, c, x);
-      grad_chunk<T>(a, g, c, x, kMask ? mask_bits<T>(mask, c) : 0u, kMask);
-      store_any<T>(a, to, c, x);
+      T::unpack(w[u], x);
+      grad_chunk<T>(a, g, c + u * kThreads, x, bits[u], kMask);
+      __builtin_nontemporal_store(T::pack(x), (typename T::chunk VL_GLOBAL *)(to + (uint64_t)(c + u * kThreads) * 16));
+    }
+    if (n_full < c1 && threadIdx.x == (n_full - c0) % kThreads) {   // the chunk that the row's end cuts
+      float x[T::kElems];
+      load_any<T>(a, row, nullptr, n_full, x);
+      grad_chunk<T>(a, g, n_full, x, kMask ? mask_bits<T>(mask, n_full) : 0u, kMask);
+      store_any<T>(a, to, n_full, x);
     }
   }
 }
@@ -1120,15 +1132,26 @@ void launch_scores(const Rows &a, const Scores &out, uint32_t n_chunk, Split spl
 
 template <class T>
 void launch_grad(const Rows &a, const Grad &b, uint32_t n_chunk, hipStream_t stream) {
-  if (n_chunk <= kShortGradChunks) {
+  // (rows of 1,500 bf16 logits, us this way / in pieces: 100 rows 4.7 / 3.5, 1,000 5.1 / 4.6, 2,500 6.9 / 7.5, 25,600 34 / 59)
+  if (n_chunk <= 128 || (n_chunk <= kShortGradChunks && a.n_row >= 2048)) {
     const uint32_t team = n_chunk <= 32 ? 16 : n_chunk <= 64 ? 32 : 64, teams = kThreads / team;
     (n_chunk <= 16 ? k_grad_short<T, 16, 1> : n_chunk <= 32 ? k_grad_short<T, 16, 2> : n_chunk <= 64 ? k_grad_short<T, 32, 2>
      : n_chunk <= 128 ? k_grad_short<T, 64, 2> : k_grad_short<T, 64, 4>)<<<std::min((a.n_row + teams - 1) / teams, 2048u), kThreads, 0, stream>>>(a, b);
     return;
   }
-  const uint32_t piece = kBatch * kThreads;
-  const dim3 grid((n_chunk + piece - 1) / piece, std::min(a.n_row, kMostGridY));
-  (a.mask ? k_grad_long<T, true> : k_grad_long<T, false>)<<<grid, kThreads, 0, stream>>>(a, b, piece);
+  // Two chunks per thread, four where a row is one piece then (us, this way / the other): 8,192 bf16 rows of 5,000 26.6 / 30.1, of 8,200 53.8 / 61.3, of
+  // 131,072 670 / 735; but 4,096 of 50,001 153 / 144.  One chunk 218 to 930 there, three 144 to 783, eight slower too.
+  // Logits that with their gradient are more than the Infinity Cache holds (256 MB) are not kept in the caches: 4,096 rows of 50,001
+  // in 32 bits 284 -> 269, 8,192 bf16 rows of 12,000 69.6 -> 67.7; but 2,000 of 20,000 (160 MB) 26.9 -> 30.4.
+  const bool once = 2ull * a.n_row * a.n_vocab * sizeof(typename T::type) > (256ull << 20);
+  auto launch = [&](auto batch) {
+    constexpr uint32_t kBatch = decltype(batch)::value;
+    const dim3 grid((n_chunk + kBatch * kThreads - 1) / (kBatch * kThreads), std::min(a.n_row, kMostGridY));
+    (a.mask ? once ? k_grad_long<T, true, true, kBatch> : k_grad_long<T, true, false, kBatch> : once ? k_grad_long<T, false, true, kBatch> : k_grad_long<T, false, false, kBatch>)
+        <<<grid, kThreads, 0, stream>>>(a, b);
+  };
+  if (n_chunk > 2 * kThreads && n_chunk <= 4 * kThreads) launch(std::integral_constant<uint32_t, 4>{});
+  else launch(std::integral_constant<uint32_t, 2>{});
 }
 
 }  // namespace
