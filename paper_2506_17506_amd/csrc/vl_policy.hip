@@ -117,6 +117,8 @@ struct Part { double loss, kl; uint64_t n_token, n_clipped; };
 constexpr uint32_t kGroups = 2, kStep = kGroups * 256;   // a lane takes kGroups times four tokens, a wavefront kStep, at once
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
+// Whole steps' numbers are not kept in the caches, read or written: 66 M tokens 162 -> 147 us, 2 M 16.3 -> 13.9; but 5 M with a reference 22.2 -> 23.4.
+__device__ inline f32x4 load_once(const float VL_GLOBAL *x) { return __builtin_nontemporal_load((const f32x4_any VL_GLOBAL *)x); }
 
 // exp(q) - q - 1 and exp(q) - 1.  Near 0 from the series of the first, q^2 (1/2 + q/6 + ... + q^7/362880), whose next term is
 // below 2^-28 of the sum for |q| < 1/2: the difference would cancel.
@@ -190,16 +192,16 @@ __global__ __launch_bounds__(kWaves * 64) void k_policy(Batch b, Part VL_GLOBAL 
       if (i >= s.from && i + kStep <= s.to) {
 #pragma unroll
         for (uint32_t u = 0; u < kGroups; ++u) {
-          lp[u] = *(const f32x4_any VL_GLOBAL *)(b.logprob + at + u * 256);
-          old[u] = *(const f32x4_any VL_GLOBAL *)(b.logprob_old + at + u * 256);
-          if (kRef) ref[u] = *(const f32x4_any VL_GLOBAL *)(b.logprob_ref + at + u * 256);
+          lp[u] = load_once(b.logprob + at + u * 256);
+          old[u] = load_once(b.logprob_old + at + u * 256);
+          if (kRef) ref[u] = load_once(b.logprob_ref + at + u * 256);
         }
 #pragma unroll
         for (uint32_t u = 0; u < kGroups; ++u) {
           f32x4 g;
 #pragma unroll
           for (uint32_t j = 0; j < 4; ++j) g[j] = token(lp[u][j], old[u][j], ref[u][j]);
-          *(f32x4_any VL_GLOBAL *)(b.grad + at + u * 256) = g;
+          __builtin_nontemporal_store(g, (f32x4_any VL_GLOBAL *)(b.grad + at + u * 256));
         }
       } else {
 #pragma unroll
@@ -282,8 +284,8 @@ int32_t check_batch(const vl_policy_batch *b) {
 }
 
 // Slices of a sample, of about 2,048 tokens by the longest one, less where that leaves wavefronts idle, and workgroups for them,
-// 8,192 at most.  (1,600 samples of 43,000 tokens on average, a slice per wavefront: 163 us; 2,048 workgroups that
-// take a slice after the other 173, slices of 4,096 tokens 168, of 1,024 179.)
+// 8,192 at most.  (1,600 samples of 43,000 tokens on average, a slice per wavefront: 147 us, slices of 4,096 tokens 156, of 1,024 142; but
+// 40 M tokens 92, 97 and 97.)
 // A workgroup of 1,024 threads alone, with nothing to join, takes what is small: two slices per wavefront at most.  (Four
 // samples, us alone / joined: 1,000 tokens 5.4 / 8.4, 16,000 7.6 / 9.0, 32,000 13.0 / 9.2; 100 samples of 1,000 in all 15.9 / 8.5.)
 constexpr uint32_t kAloneTokens = 16384, kAloneSlices = 32;
