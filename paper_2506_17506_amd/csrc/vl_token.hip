@@ -389,7 +389,7 @@ __device__ inline void write_top(const Scores &out, uint32_t r, uint32_t k, uint
   if (out.top_token) out.top_token[at] = key && !f.bad ? (int32_t)~(uint32_t)key : -1;
   if (out.top_logprob) out.top_logprob[at] = f.bad ? f.s : key ? logprob_of(f, unordered<T>((uint32_t)(key >> 32))) : kNoLogit;
 }
-// a row of padding; `lane` of 64 or more
+// a row of padding; `lane` of out.n_top or more
 __device__ inline void write_padding(const Scores &out, uint32_t r, uint32_t lane) {
   if (lane == 0) {
     if (out.logprob) out.logprob[r] = 0.0f;
@@ -1105,6 +1105,7 @@ void launch_scores(const Rows &a, const Scores &out, uint32_t n_chunk, Split spl
   // 256, four 12.8 / 15.9, eight 19.0 / 16.7.  An alternative more takes 0.35 to 0.85 us even of few rows, where the search's take
   // 0.05 (one alternative of 500 rows of 512 3.95 / 3.92, two 4.8 / 4.0; of 4,000 rows two 4.86 / 4.86; four of rows of 256, 4,000 of
   // them 5.0 / 5.0, 8,000 5.6 / 7.2; eight of rows of 128, 4,000 of them 5.6 / 5.3, 8,000 6.1 / 7.6).
+  // (16 at most, as many as a row has lanes)
   const uint32_t held = (n_chunk <= 16 ? 1u : n_chunk <= 32 ? 2u : 4u) * T::kElems;   // logits of a lane
   if (n_chunk <= kShortChunks && (out.n_top <= 1 || (out.n_top * held <= 64 && a.n_row >= 512 * (out.n_top + 5)))) {
     // 16 lanes per row while a lane has at most 4 chunks, then 32.  25,600 bf16 rows of 512: 9.6 us with 16 lanes, 10.1 with
