@@ -154,20 +154,6 @@ __device__ inline uint32_t mask_bits(const uint8_t VL_GLOBAL *mask, uint32_t lea
   return (uint32_t)mask[c] << 1 | (c ? mask[c - 1] >> 7 : 0u);   // (nothing allowed in front of the row)
 }
 
-// chunk c of a row of n logits, of which the row's end may cut some off: those are -infinity
-template <class T>
-__device__ inline void load_any(const Rows &a, const uint8_t VL_GLOBAL *row, const uint8_t VL_GLOBAL *mask, uint32_t c, float *x) {
-  const uint32_t from = c * T::kElems;
-  if (from + T::kElems <= a.n_vocab) {
-    T::unpack(load_chunk<T>(row, c), x);
-  } else {
-#pragma unroll
-    for (uint32_t j = 0; j < T::kElems; ++j)
-      x[j] = from + j < a.n_vocab ? T::wide(((const typename T::type VL_GLOBAL *)row)[from + j]) : kNoLogit;
-  }
-  if (mask) keep_allowed<T>(x, from < a.n_vocab ? mask_bits<T>(mask, c) : 0u);
-}
-
 // Chunks lane, lane + kStride, ... of a short row, into bits what the mask says of them (all ones without one).  All loads are on their way
 // before the first is waited for.
 template <class T, uint32_t kStride, uint32_t kChunks>
@@ -745,7 +731,7 @@ __global__ __launch_bounds__(kTeam, kTeam == 1024 && kN == 2 ? 8 : 1) void k_sco
       if (lead > c) x[0][0] = kNoLogit;
       add(std::integral_constant<uint32_t, kN>{}, x, c, w, bits);
     }
-    if (n_full < c1 && threadIdx.x == (n_full - c0) % kTeam) {   // the chunk that the row's end cuts
+    if (c0 <= n_full && n_full < c1 && threadIdx.x == (n_full - c0) % kTeam) {   // the chunk that the row's end cuts
       float x[1][T::kElems];
       load_any<T>(a, row, mask, lead, n_full, x[0]);
       const u32x4 w = kOne ? T::pack(x[0]) : u32x4{};   // (as it was: these are the type's own values)
@@ -905,15 +891,16 @@ __device__ inline GradRow grad_row(const Rows &a, const Grad &b, uint32_t r) {
   return g;
 }
 template <class T>
-__device__ inline void grad_chunk(const Rows &a, const GradRow &g, uint32_t c, float *x, uint32_t bits, bool masked) {
+__device__ inline void grad_chunk(const Rows &a, const GradRow &g, uint32_t lead, uint32_t c, float *x, uint32_t bits, bool masked) {
 #pragma unroll
   for (uint32_t j = 0; j < T::kElems; ++j) {
     const float t = __builtin_fmaf(x[j] - g.ref, a.scale2, -g.log2_sum), p = __builtin_amdgcn_exp2f(t);
     x[j] = p * __builtin_fmaf(fmaxf(t, kFar), g.slope, g.level);
   }
-  if (g.token / T::kElems == c) {
+  const uint32_t place = g.token + lead;
+  if (place / T::kElems == c) {
 #pragma unroll
-    for (uint32_t j = 0; j < T::kElems; ++j) x[j] += g.token % T::kElems == j ? g.hot : 0.0f;
+    for (uint32_t j = 0; j < T::kElems; ++j) x[j] += place % T::kElems == j ? g.hot : 0.0f;
   }
   if (masked) {   // 0 where not allowed, whatever stood there
 #pragma unroll
@@ -953,7 +940,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_short(Rows a, Grad b) {
     const GradRow g = grad_row(a, b, r);
 #pragma unroll
     for (uint32_t i = 0; i < kChunks; ++i) {
-      grad_chunk<T>(a, g, lane + kTeam * i, x[i], bits[i], mask != nullptr);
+      grad_chunk<T>(a, g, 0, lane + kTeam * i, x[i], bits[i], mask != nullptr);
 #pragma unroll
       for (uint32_t j = 0; j < T::kElems; ++j) x[i][j] = g.idle ? 0.0f : x[i][j];
       store_any<T>(a, to, lane + kTeam * i, x[i]);
@@ -965,19 +952,24 @@ __global__ __launch_bounds__(kThreads) void k_grad_short(Rows a, Grad b) {
 template <class T, bool kMask, bool kOnce, uint32_t kBatch>
 __global__ __launch_bounds__(kThreads) void k_grad_long(Rows a, Grad b) {
   constexpr uint32_t piece_chunks = kBatch * kThreads;
-  const uint32_t n_full = a.n_vocab / T::kElems, n_chunk = (a.n_vocab + T::kElems - 1) / T::kElems;
-  const uint32_t c0 = blockIdx.x * piece_chunks, c1 = min(n_chunk, c0 + piece_chunks), c1_full = min(n_full, c1);
+  typedef typename T::chunk chunk;
+  const uint32_t c0 = blockIdx.x * piece_chunks, c = c0 + threadIdx.x;
   for (uint32_t r = blockIdx.y; r < a.n_row; r += gridDim.y) {
     const uint8_t VL_GLOBAL *row = a.logits + (uint64_t)r * a.ld;
     uint8_t VL_GLOBAL *to = b.grad + (uint64_t)r * b.ld;
     const uint8_t VL_GLOBAL *mask = kMask ? a.mask + (uint64_t)r * a.mask_ld : nullptr;
     const GradRow g = grad_row(a, b, r);
-    uint32_t c = c0 + threadIdx.x;
+    // (chunks from the even place in front, if that suits both: 4,096 bf16 rows of 50,001 151 -> 142 us, 25,600 of 20,011 392 -> 359)
+    const uint32_t lead = lead_of<T>(row) == lead_of<T>(to) ? lead_of<T>(row) : 0u;
+    const uint32_t n_full = (a.n_vocab + lead) / T::kElems, n_chunk = (a.n_vocab + lead + T::kElems - 1) / T::kElems;
+    const uint32_t c1 = min(n_chunk, c0 + piece_chunks), c1_full = min(n_full, c1);
     if (g.idle) {
       float x[T::kElems] = {};
-      for (; c < c1; c += kThreads) store_any<T>(a, to, c, x);
+      for (uint32_t at = c; at < c1; at += kThreads) store_any<T>(a, to, at, x);
       continue;
     }
+    row -= lead * 2;
+    to -= lead * 2;
     u32x4 w[kBatch];
     uint32_t bits[kBatch];
     const bool all = c0 + piece_chunks <= c1_full;
@@ -989,21 +981,32 @@ __global__ __launch_bounds__(kThreads) void k_grad_long(Rows a, Grad b) {
 #pragma unroll
     for (uint32_t u = 0; u < kBatch; ++u) {
       bits[u] = 0;
-      if (kMask && (all || c + u * kThreads < c1_full)) bits[u] = mask_bits<T>(mask, c + u * kThreads);
+      if (kMask && (all || c + u * kThreads < c1_full)) bits[u] = mask_bits<T>(mask, lead, c + u * kThreads);
     }
 #pragma unroll
     for (uint32_t u = 0; u < kBatch; ++u) {
-      if (!all && c + u * kThreads >= c1_full) break;
+      const uint32_t at = c + u * kThreads;
+      if (!all && at >= c1_full) break;
       float x[T::kElems];
       T::unpack(w[u], x);
-      grad_chunk<T>(a, g, c + u * kThreads, x, bits[u], kMask);
-      __builtin_nontemporal_store(T::pack(x), (typename T::chunk VL_GLOBAL *)(to + (uint64_t)(c + u * kThreads) * 16));
+      grad_chunk<T>(a, g, lead, at, x, bits[u], kMask);
+      if (lead > at) {   // (what stands in front of the row stays)
+        for (uint32_t j = 1; j < T::kElems; ++j) ((typename T::type VL_GLOBAL *)to)[j] = T::narrow(x[j]);
+      } else {
+        __builtin_nontemporal_store(T::pack(x), (chunk VL_GLOBAL *)(to + (uint64_t)at * 16));
+      }
     }
-    if (n_full < c1 && threadIdx.x == (n_full - c0) % kThreads) {   // the chunk that the row's end cuts
+    if (c0 <= n_full && n_full < c1 && threadIdx.x == (n_full - c0) % kThreads) {   // the chunk that the row's end cuts
       float x[T::kElems];
-      load_any<T>(a, row, nullptr, n_full, x);
-      grad_chunk<T>(a, g, n_full, x, kMask ? mask_bits<T>(mask, n_full) : 0u, kMask);
-      store_any<T>(a, to, n_full, x);
+      load_any<T>(a, row + lead * 2, nullptr, lead, n_full, x);
+      grad_chunk<T>(a, g, lead, n_full, x, 0, false);
+#pragma unroll
+      for (uint32_t j = 0; j < T::kElems; ++j) {
+        const uint32_t t = n_full * T::kElems + j - lead;
+        if (t >= a.n_vocab) continue;   // (behind the row, or in front of it)
+        const bool allowed = !kMask || ((mask[t >> 3] >> (t & 7)) & 1);
+        ((typename T::type VL_GLOBAL *)(to + lead * 2))[t] = T::narrow(allowed ? x[j] : 0.0f);
+      }
     }
   }
 }
@@ -1141,13 +1144,15 @@ void launch_grad(const Rows &a, const Grad &b, uint32_t n_chunk, hipStream_t str
     return;
   }
   // Two chunks per thread, four where a row is one piece then (us, this way / the other): 8,192 bf16 rows of 5,000 26.6 / 30.1, of 8,200 53.8 / 61.3, of
-  // 131,072 670 / 735; but 4,096 of 50,001 153 / 144.  One chunk 218 to 930 there, three 144 to 783, eight slower too.
+  // 131,072 670 / 735.  One chunk 930 there, three 783, eight 781.
   // Logits that with their gradient are more than the Infinity Cache holds (256 MB) are not kept in the caches: 4,096 rows of 50,001
   // in 32 bits 284 -> 269, 8,192 bf16 rows of 12,000 69.6 -> 67.7; but 2,000 of 20,000 (160 MB) 26.9 -> 30.4.
+  const bool lead = T::kElems == 8 && (((uintptr_t)a.logits | (a.n_row > 1 ? a.ld : 0)) & 2);   // some row starts at an odd place
+  const uint32_t n_most = (a.n_vocab + lead + T::kElems - 1) / T::kElems;
   const bool once = 2ull * a.n_row * a.n_vocab * sizeof(typename T::type) > (256ull << 20);
   auto launch = [&](auto batch) {
     constexpr uint32_t kBatch = decltype(batch)::value;
-    const dim3 grid((n_chunk + kBatch * kThreads - 1) / (kBatch * kThreads), std::min(a.n_row, kMostGridY));
+    const dim3 grid((n_most + kBatch * kThreads - 1) / (kBatch * kThreads), std::min(a.n_row, kMostGridY));
     (a.mask ? once ? k_grad_long<T, true, true, kBatch> : k_grad_long<T, true, false, kBatch> : once ? k_grad_long<T, false, true, kBatch> : k_grad_long<T, false, false, kBatch>)
         <<<grid, kThreads, 0, stream>>>(a, b);
   };

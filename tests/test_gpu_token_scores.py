@@ -209,6 +209,36 @@ def test_windows_of_wider_rows(dtype, n, v, first, after):
     assert full[:, :first].isnan().all() and full[:, first + v:].isnan().all()
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("v", [4095, 4096, 4097, 8190, 8191, 8192, 8193, 16384, 2056, 2087])
+@pytest.mark.parametrize("masked", [False, True])
+def test_gradient_at_the_ends_of_long_rows(v, dtype, masked):
+    """rows at odd and even places whose chunks fill pieces to the last one, or one more or less; beside them, in place, and from the other parity"""
+    n = 4
+    t = torch.tensor([0, v - 1, v // 2, 7], dtype=torch.int32).cuda()
+    mask = words_of(some_bits(n, v, 3)).cuda() if masked else None   # (no word more than the row needs)
+    for first, pitch in ((0, v + 1), (1, v + 2), (1, v + 1)):
+        full = torch.full((n * pitch + first + 9,), 7.0, dtype=dtype, device="cuda")
+        x = full.as_strided((n, v), (pitch, 1), first)
+        x.copy_(bell(n, v, dtype, v))
+        out = scores(x, t, mask)
+        want = Rows(x, t, mask)
+        g, e = torch.tensor([1.0, -2.0, 0.5, 3.0]), torch.tensor([0.5, 1.0, -1.0, 0.0])
+        d, err = want.grad(dtype, g, e)
+        args = dict(token=t, mask=mask, entropy=out["entropy"], g_logprob=g.cuda(), g_entropy=e.cuda())
+        beside = torch.ones(full.shape, dtype=torch.bool, device="cuda")
+        beside.as_strided((n, v), (pitch, 1), first)[:] = False
+        for shift in (0, 1):
+            side = torch.full_like(full, 7.0)
+            to = side.as_strided((n, v), (pitch, 1), first + shift)
+            vl.vl_token_logprobs_grad(x, out["stat"], to, **args)
+            near(to, d, err, f"start {first}, pitch {pitch}, shift {shift}")
+            assert (side[shift:][beside[:len(side) - shift]] == 7.0).all() and (side[:shift] == 7.0).all()
+        vl.vl_token_logprobs_grad(x, out["stat"], x, **args)
+        near(x, d, err, "in place")
+        assert (full[beside] == 7.0).all()
+
+
 @pytest.mark.parametrize("n,v", [(4, 512), (4, 3001), (1, 70000)])
 def test_one_mask_for_all_rows(n, v):
     x, t = bell(n, v, BF16, 3), tokens(n, v, 4)
