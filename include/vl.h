@@ -434,7 +434,8 @@ int32_t vl_group_advantages(const vl_counts *counts, const float *extra, uint32_
  *   grad_t = weight[c] * ( -a * exp(d), or 0 if clipped, + kl * (1 - exp(q)) )
  *   loss   = sum over c of weight[c] * sum over its tokens of loss_t; stats->kl the same of kl_t
  * (weight: 1 / tokens of all samples, or 1 / (samples * len[c]), as the caller averages.)  A term whose factor a, kl or weight is 0 is
- * 0; exp is taken in 32 bits, so that other terms are infinite where it is above 88.7.  d is compared with the
+ * 0; exp is taken in 32 bits, so that other terms are infinite where its argument is above 88.7.  So is kl_t where one of logprob
+ * and logprob_ref is -infinity, a token that a mask takes out in one of them; a difference of two equal infinities is NaN.  d is compared with the
  * bounds in 64 bits; sums are joined in 64 bits in an order that the sizes alone decide.  grad is written at the samples'
  * tokens only and may be logprob itself.  Tokens at n or above are not touched, and stats->n_token leaves them out.
  * max_len: the longest sample, as near as the host knows it: it decides the launch's shape alone.

@@ -121,7 +121,7 @@ typedef f32x4 f32x4_any __attribute__((aligned(4)));
 __device__ inline f32x4 load_once(const float VL_GLOBAL *x) { return __builtin_nontemporal_load((const f32x4_any VL_GLOBAL *)x); }
 
 // exp(q) - q - 1 and exp(q) - 1.  Near 0 from the series of the first, q^2 (1/2 + q/6 + ... + q^7/362880), whose next term is
-// below 2^-28 of the sum for |q| < 1/2: the difference would cancel.
+// below 2^-28 of the sum for |q| < 1/2: the difference would cancel.  Infinite where the exponential is, at q = +infinity too.
 __device__ inline void exp_gap(float q, float &gap, float &less_one) {
   if (fabsf(q) < 0.5f) {
     gap = q * q * (0.5f + q * (1.0f / 6 + q * (1.0f / 24 + q * (1.0f / 120 + q * (1.0f / 720 + q * (1.0f / 5040 + q * (1.0f / 40320 + q * (1.0f / 362880))))))));
@@ -129,7 +129,7 @@ __device__ inline void exp_gap(float q, float &gap, float &less_one) {
   } else {
     const float e = expf(q);
     less_one = e - 1.0f;
-    gap = less_one - q;
+    gap = e == __builtin_huge_valf() ? e : less_one - q;
   }
 }
 

@@ -1,0 +1,67 @@
+"""Advantages and the policy loss where numbers are infinite or missing, on the GPU: what is left of the others."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import paper_2506_17506_amd as vl  # noqa: E402
+from test_gpu_policy_loss import call, device, make  # noqa: E402
+from token_reference import U, near, policy  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    vl.load()
+
+
+@pytest.mark.parametrize("kl", [0.1, 0.0])
+@pytest.mark.parametrize("m,n_tok", [(3, 7), (3, 600), (100, 700)])   # (one launch, and parts that are joined)
+def test_a_token_that_the_model_cannot_emit_against_a_reference(m, n_tok, kl):
+    """logprob -infinity, the reference finite: q = +infinity, exp(q) - q - 1 and exp(q) are infinite, and no other token's
+    gradient is touched"""
+    b = make([k * n_tok for k in range(m)], [n_tok] * m, m * n_tok, 11)
+    b["adv"][:2], b["weight"][:2] = (1.5, -0.5), (0.25, 0.125)
+    args = (b["start"], b["length"], b["adv"], b["weight"], -0.25, 0.25, kl)
+    g, err = policy(b["lp"], b["old"], b["ref"], *args)[:2]
+    at = [2, n_tok + 3]
+    b["lp"][at] = -np.inf
+    b["old"][at] = -1.0
+    tokens, clipped = policy(b["lp"], b["old"], None, *args)[6:]
+    d = device(b)
+    grad, stats = torch.full_like(d["lp"], 77.0), torch.zeros(24, dtype=torch.uint8, device="cuda")
+    call(d, grad, stats, kl=kl)
+    s = stats.cpu().numpy().view(vl.POLICY_STATS_DTYPE)[0]
+    assert (s["n_token"], s["n_clipped"]) == (tokens, clipped)
+    assert s["kl"] == np.inf
+    got = grad.cpu().numpy()
+    if kl:
+        assert s["loss"] == np.inf
+        assert (got[at] == -np.inf).all()
+    else:   # (the distance is only reported; exp(d) is 0 there, and the second's ratio is below the bound)
+        some = [np.delete(b[k], at) for k in ("lp", "old")]
+        short = b["length"].copy()
+        short[:2] -= 1
+        loss, loss_err = policy(*some, None, short.cumsum() - short, short, *args[2:])[2:4]
+        clip = float(b["weight"][1]) * 0.5 * np.exp(-0.25)   # (what the second one adds: one rounding and the exponential's)
+        assert abs(s["loss"] - (loss + clip)) <= loss_err + clip * 2.0 ** -20 + U * abs(loss + clip) and (got[at] == 0).all()
+    others = np.ones(m * n_tok, bool)
+    others[at] = False
+    near(grad[torch.from_numpy(others).cuda()], g[others], err[others], "the others' gradient")
+
+
+@pytest.mark.parametrize("n_tok", [7, 700])
+def test_a_token_that_the_reference_cannot_emit(n_tok):
+    """q = -infinity: exp(q) - q - 1 is infinite, exp(q) is 0"""
+    m = 3
+    b = make([k * n_tok for k in range(m)], [n_tok] * m, m * n_tok, 12)
+    b["adv"][0], b["weight"][0] = 0.0, 0.25
+    b["ref"][2] = -np.inf
+    d = device(b)
+    grad, stats = torch.full_like(d["lp"], 77.0), torch.zeros(24, dtype=torch.uint8, device="cuda")
+    call(d, grad, stats, kl=0.5)
+    s = stats.cpu().numpy().view(vl.POLICY_STATS_DTYPE)[0]
+    assert s["loss"] == np.inf and s["kl"] == np.inf and grad[2].item() == 0.125 and grad.isfinite().all()
