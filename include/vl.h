@@ -413,7 +413,8 @@ int32_t vl_token_logprobs_grad(const vl_token_rows *rows, const float *stat, con
  * group, usually the K samples of one program:
  *   reward    = extra + ok * (kinds == 0) + cons * n_cons + real * n_real + safe * n_safe
  *   advantage = (reward - mean of its group) / (standard deviation of its group, over its size, + eps)
- * in 64 bits, rounded once; groups of one sample or of equal rewards have advantage 0.
+ * in 64 bits, rounded once; groups of one sample or of equal rewards have advantage 0.  A reward that is infinite or NaN (extra's)
+ * makes every advantage of its group NaN.
  * counts [device] as vl_count_violations_multi writes them, may be NULL if extra is not (their terms are 0 then);
  * extra [device] [n], may be NULL: any other reward, say of vl_bank_conflicts; group_off [device] [n_group + 1]: samples
  * group_off[g] .. group_off[g + 1] - 1, non-decreasing; what lies at n or above is not touched.

@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kTeam < 256 ? 256 : kTeam) void k_advantages(Reward
       v += d * d;
     }
     team_sums<kTeam>(s, v, room);
-    const double mean = s / size, scale = 1.0 / (sqrt(fmax(v / size - mean * mean, 0.0)) + eps);
+    const double mean = s / size, var = v / size - mean * mean, scale = 1.0 / (sqrt(var < 0.0 ? 0.0 : var) + eps);   // (NaN stays NaN)
 #pragma unroll
     for (uint32_t i = 0; i < kKeep; ++i) {
       const uint64_t k = (uint64_t)k0 + me + i * kTeam;

@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2506_17506_amd as vl  # noqa: E402
 from test_gpu_policy_loss import call, device, make  # noqa: E402
-from token_reference import U, near, policy  # noqa: E402
+from token_reference import U, advantages, near, policy  # noqa: E402
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -65,3 +65,21 @@ def test_a_token_that_the_reference_cannot_emit(n_tok):
     call(d, grad, stats, kl=0.5)
     s = stats.cpu().numpy().view(vl.POLICY_STATS_DTYPE)[0]
     assert s["loss"] == np.inf and s["kl"] == np.inf and grad[2].item() == 0.125 and grad.isfinite().all()
+
+
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("k", [2, 100, 300, 1025, 5000])   # (a wavefront, 256 and 1,024 threads per group; more than their registers hold)
+@pytest.mark.parametrize("where", [0, 1, -1])
+def test_a_reward_that_is_not_finite(k, where, bad):
+    """mean and deviation of its group are not numbers, so neither is any of the group's advantages, wherever it stands; other
+    groups keep theirs"""
+    rng = np.random.default_rng(k)
+    extra = rng.standard_normal(3 * k).astype(np.float32)
+    extra[k:2 * k][where] = bad
+    off = torch.tensor([0, k, 2 * k, 3 * k], dtype=torch.int32, device="cuda")
+    reward, adv = torch.full((3 * k,), 77.0, device="cuda"), torch.full((3 * k,), 77.0, device="cuda")
+    vl.vl_group_advantages(None, off, (1.0, 0.0, 0.0, 0.0), 1e-6, adv, reward=reward, extra=torch.from_numpy(extra).cuda())
+    assert np.array_equal(reward.cpu().numpy(), extra, equal_nan=True)
+    assert adv[k:2 * k].isnan().all()
+    _, want = advantages(None, np.delete(extra, np.arange(k, 2 * k)), [0, k, 2 * k], (1.0, 0.0, 0.0, 0.0), 1e-6)
+    near(torch.cat([adv[:k], adv[2 * k:]]), want, U * np.abs(want) + 2.0 ** -20, "the other groups")
