@@ -434,7 +434,8 @@ int32_t vl_group_advantages(const vl_counts *counts, const float *extra, uint32_
  *   loss_t = -a * exp(d), or with the bound in place of d if clipped, + kl * kl_t
  *   grad_t = weight[c] * ( -a * exp(d), or 0 if clipped, + kl * (1 - exp(q)) )
  *   loss   = sum over c of weight[c] * sum over its tokens of loss_t; stats->kl the same of kl_t
- * (weight: 1 / tokens of all samples, or 1 / (samples * len[c]), as the caller averages.)  A term whose factor a, kl or weight is 0 is
+ * (weight: 1 / tokens of all samples, or 1 / (samples * len[c]), as the caller averages; that of a sample without tokens counts
+ * for nothing, whatever it is.)  A term whose factor a, kl or weight is 0 is
  * 0; exp is taken in 32 bits, so that other terms are infinite where its argument is above 88.7.  So is kl_t where one of logprob
  * and logprob_ref is -infinity, a token that a mask takes out in one of them; a difference of two equal infinities is NaN.  d is compared with the
  * bounds in 64 bits; sums are joined in 64 bits in an order that the sizes alone decide.  grad is written at the samples'

@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_policy(Batch b, Part VL_GLOBAL 
           }
       }
     }
-    if (s.w != 0.0f) {
+    if (s.w != 0.0f && s.from < s.to) {   // (the weight of a sample without tokens may be 1 / 0)
       loss += (double)s.w * sum;
       if (kRef) kls += (double)s.w * kl_sum;
     }

@@ -7,7 +7,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 import paper_2506_17506_amd as vl  # noqa: E402
-from test_gpu_policy_loss import call, device, make  # noqa: E402
+from test_gpu_policy_loss import call, check_out, device, make  # noqa: E402
 from token_reference import U, advantages, near, policy  # noqa: E402
 
 
@@ -83,3 +83,21 @@ def test_a_reward_that_is_not_finite(k, where, bad):
     assert adv[k:2 * k].isnan().all()
     _, want = advantages(None, np.delete(extra, np.arange(k, 2 * k)), [0, k, 2 * k], (1.0, 0.0, 0.0, 0.0), 1e-6)
     near(torch.cat([adv[:k], adv[2 * k:]]), want, U * np.abs(want) + 2.0 ** -20, "the other groups")
+
+
+@pytest.mark.parametrize("odd", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("m,n_tok,max_len", [(4, 9, None), (4, 9, 30000), (40, 1100, None)])   # (one workgroup, many slices, parts that are joined)
+def test_weights_of_samples_without_tokens(m, n_tok, max_len, odd):
+    """weight = 1 / (samples * len) is infinite for a sample that was stopped before its first token, or lies past the arrays: it adds
+    nothing"""
+    length = np.full(m, n_tok)
+    length[[0, m - 1]] = 0
+    start = length.cumsum() - length
+    start[1], b_n = 2 ** 40, int(length.sum())   # (the second sample's tokens are not there)
+    b = make(start, length, b_n, 13)
+    b["adv"][[0, 1, m - 1]] = (1.0, -1.0, 0.0)
+    b["weight"][[0, 1, m - 1]] = odd
+    d = device(b)
+    grad, stats = torch.full_like(d["lp"], 77.0), torch.full((24,), 255, dtype=torch.uint8, device="cuda")
+    call(d, grad, stats, max_len=max_len)
+    check_out(b, grad, stats)
