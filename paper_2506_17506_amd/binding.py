@@ -566,14 +566,14 @@ def vl_group_advantages(counts, group_off, weights, eps, advantage, reward=None,
     some = advantage if advantage is not None else reward if reward is not None else extra
     if some is None:
         raise VlError(-1, what)
-    shape, n, f = some.shape, some.numel(), _t.f32
-    if not n:
+    shape, n, n_group, f = some.shape, some.numel(), max(0, group_off.numel() - 1), _t.f32
+    if not n or n >> 31 or n_group >> 31:   # (the arguments of 32 bits would take the low ones)
         raise VlError(-2, what)
     p = _tensor(what, counts, _t.record[:3], None, device)
     if counts is not None and counts.numel() * counts.element_size() != 32 * n:
         raise VlError(-2, what)
     rc = _lib.vl_group_advantages(p, _tensor(what, extra, f, shape, device), n, _tensor(what, group_off, _t.words, None, device),
-                                  max(0, group_off.numel() - 1), _packed(what, _WEIGHTS, *weights), eps, _tensor(what, reward, f, shape, device),
+                                  n_group, _packed(what, _WEIGHTS, *weights), eps, _tensor(what, reward, f, shape, device),
                                   _tensor(what, advantage, f, shape, device), _call_stream(stream, device))
     if rc != 0:
         raise VlError(rc, what)
