@@ -171,6 +171,13 @@ def _stream_ptr(stream):
     return C.c_void_p(int(getattr(stream, "cuda_stream", stream)))
 
 
+def _u32(what, x, code=-2):
+    """a size that a field or an argument of 32 bits holds (of others ctypes would take the low bits)"""
+    if x >> 32:
+        raise VlError(code, what)
+    return x
+
+
 def make_desc(m):
     """(desc, keepalive) for any object with the array attributes of a program
     description (blk_start, succ_off, succ, instr_occ_off, occ_vreg, occ_flags,
@@ -241,7 +248,7 @@ def vl_mir_lanes_get(mir) -> dict:
 
 def vl_lanes_expand(mir, cand, K: int, ld: int, cand_low, ld_low: int, stream=None) -> None:
     """cand, cand_low: device pointers or tensors of uint16 rows."""
-    rc = load().vl_lanes_expand(mir, C.c_void_p(_dev_ptr(cand)), K, ld, C.c_void_p(_dev_ptr(cand_low)), ld_low,
+    rc = load().vl_lanes_expand(mir, C.c_void_p(_dev_ptr(cand)), _u32("vl_lanes_expand", K), ld, C.c_void_p(_dev_ptr(cand_low)), ld_low,
                                 _stream_ptr(stream))
     if rc != 0:
         raise VlError(rc, "vl_lanes_expand")
@@ -285,7 +292,7 @@ def vl_live_get(live) -> _View:
 
 def vl_verify_batch(mir, live, cand, K: int, ld: int, out, stream=None) -> None:
     """cand, out: device pointers (int) or torch tensors."""
-    rc = load().vl_verify_batch(mir, live, C.c_void_p(_dev_ptr(cand)), K, ld, C.c_void_p(_dev_ptr(out)),
+    rc = load().vl_verify_batch(mir, live, C.c_void_p(_dev_ptr(cand)), _u32("vl_verify_batch", K), ld, C.c_void_p(_dev_ptr(out)),
                                 _stream_ptr(stream))
     if rc != 0:
         raise VlError(rc, "vl_verify_batch")
@@ -293,7 +300,7 @@ def vl_verify_batch(mir, live, cand, K: int, ld: int, out, stream=None) -> None:
 
 def vl_verify_batch_static(mir, live, cand, K: int, ld: int, out, stream=None) -> None:
     """vl_verify_batch without any allocation inside the library."""
-    rc = load().vl_verify_batch_static(mir, live, C.c_void_p(_dev_ptr(cand)), K, ld, C.c_void_p(_dev_ptr(out)),
+    rc = load().vl_verify_batch_static(mir, live, C.c_void_p(_dev_ptr(cand)), _u32("vl_verify_batch_static", K), ld, C.c_void_p(_dev_ptr(out)),
                                        _stream_ptr(stream))
     if rc != 0:
         raise VlError(rc, "vl_verify_batch_static")
@@ -304,7 +311,7 @@ def make_jobs(jobs):
     arr = (_Job * len(jobs))()
     for i, (mir, live, cand, K, ld, out) in enumerate(jobs):
         arr[i].mir, arr[i].live = mir.value, live.value
-        arr[i].cand, arr[i].K, arr[i].ld, arr[i].out = _dev_ptr(cand), K, ld, _dev_ptr(out)
+        arr[i].cand, arr[i].K, arr[i].ld, arr[i].out = _dev_ptr(cand), _u32("make_jobs", K), ld, _dev_ptr(out)
     return arr
 
 
@@ -343,7 +350,7 @@ def vl_count_violations_multi(jobs, stream=None) -> None:
     arr = (_CountJob * len(jobs))()
     for i, (mir, live, cand, K, ld, out) in enumerate(jobs):
         arr[i].mir, arr[i].live = mir.value, live.value
-        arr[i].cand, arr[i].K, arr[i].ld, arr[i].out = _dev_ptr(cand), K, ld, _dev_ptr(out)
+        arr[i].cand, arr[i].K, arr[i].ld, arr[i].out = _dev_ptr(cand), _u32("vl_count_violations_multi", K), ld, _dev_ptr(out)
     rc = load().vl_count_violations_multi(arr, len(arr), _stream_ptr(stream))
     if rc != 0:
         raise VlError(rc, "vl_count_violations_multi")
@@ -351,7 +358,7 @@ def vl_count_violations_multi(jobs, stream=None) -> None:
 
 def vl_bank_conflicts(mir, cand, K: int, ld: int, n_banks: int, out, stream=None) -> None:
     """out: device buffer of K uint32."""
-    rc = load().vl_bank_conflicts(mir, C.c_void_p(_dev_ptr(cand)), K, ld, n_banks, C.c_void_p(_dev_ptr(out)),
+    rc = load().vl_bank_conflicts(mir, C.c_void_p(_dev_ptr(cand)), _u32("vl_bank_conflicts", K), ld, _u32("vl_bank_conflicts", n_banks, -3), C.c_void_p(_dev_ptr(out)),
                                   _stream_ptr(stream))
     if rc != 0:
         raise VlError(rc, "vl_bank_conflicts")

@@ -4,14 +4,16 @@ import torch
 
 import paper_2506_17506_amd as vl
 from paper_2506_17506_amd import binding
+from stand_in import in_own_process
+from test_host_paths import analysed, jobs_of
 
 
 class Tensor:
     """what the binding asks of a float32 or int32 tensor of n elements on device 0; there is no memory behind it"""
     is_cuda = True
 
-    def __init__(self, n, dtype=torch.float32):
-        self.n, self.dtype, self.shape = n, dtype, (n,)
+    def __init__(self, n, dtype=None):
+        self.n, self.dtype, self.shape = n, dtype or torch.float32, (n,)
 
     def get_device(self):
         return 0
@@ -49,3 +51,32 @@ def test_more_samples_or_groups_than_the_header_allows(monkeypatch, n, n_offsets
     vl.vl_group_advantages(None, Tensor(3, torch.int32), (1, 0, 0, 0), 1e-6, Tensor(2 ** 31 - 1), extra=Tensor(2 ** 31 - 1))
     (args,) = called
     assert args[2] == 2 ** 31 - 1 and args[4] == 2
+
+
+@in_own_process
+def test_candidates_that_32_bits_do_not_count(s):
+    """more than 2^32 candidates, and fewer than none"""
+    (hm,), (hl,) = analysed(s, 1)
+    jobs, keep = jobs_of(s, [hm], [hl], 8)
+    _, _, cand, _, ld, out = jobs[0]
+    for K in (2 ** 32 + 8, 2 ** 33 + 8, -1, -2 ** 32 + 8):
+        s.launches.clear()
+        for call in (lambda: s.vl.vl_verify_batch(hm, hl, cand, K, ld, out, stream=1), lambda: s.vl.vl_verify_batch_static(hm, hl, cand, K, ld, out, stream=1),
+                     lambda: s.vl.vl_verify_multi([(hm, hl, cand, K, ld, out)], stream=1), lambda: s.vl.vl_verify_multi_occ_major([(hm, hl, cand, K, ld, out)], stream=1),
+                     lambda: s.vl.vl_count_violations_multi([(hm, hl, cand, K, ld, out)], stream=1), lambda: s.vl.vl_bank_conflicts(hm, cand, K, ld, 4, out, stream=1),
+                     lambda: s.vl.vl_lanes_expand(hm, cand, K, ld, out, ld, stream=1), lambda: s.vl.vl_summarize_multi([(hm, hl, cand, K, ld, out)], out, stream=1)):
+            try:
+                call()
+            except s.vl.VlError as e:
+                assert e.code == -2, e
+            else:
+                raise AssertionError(f"{K} candidates taken")
+        assert not s.launches
+    for n_banks in (2 ** 32 + 4, -1):
+        try:
+            s.vl.vl_bank_conflicts(hm, cand, 8, ld, n_banks, out, stream=1)
+        except s.vl.VlError as e:
+            assert e.code == -3, e
+        else:
+            raise AssertionError(f"{n_banks} banks taken")
+    assert not s.launches
