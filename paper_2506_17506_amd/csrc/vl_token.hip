@@ -848,7 +848,8 @@ __global__ __launch_bounds__(kThreads) void k_scores_join(Rows a, Scores out, ui
         }
       }
       __syncthreads();
-      // (at most n_top + kMoreHot threads have such keys, with VL_MAX_TOP each at most; a part's keys are next to each other)
+      // (The bound is one of columns of kWaves threads: n_top + kMoreHot of the 64 reach `least`, so up to kWaves times as many threads, each
+      // with n_part * n_top / kThreads keys or one more.  Where that is more than there is room for, insertion finds the best.)
       uint64_t best;
       if (sh.room.n <= sh.room.kMost) {
         best = in_order(sh.room.key, sh.room.n, sh.key, n_top);
@@ -1062,6 +1063,7 @@ Rows device_rows(const vl_token_rows *a) {
 //   500 x 32,000 in 32 bits, one: 256 14.8 / 1,024 15.9;               500 x 100,000: 1,024 24.2 / 256 26.9
 //   150 x 32,000: 1,024 5.9 / 256 7.2, in 3 parts 9.2;                 1 x 32,000: 1,024 4.7 / 256 5.6
 //   1 x 131,072, twenty: 256 in 21 parts 10.2 / in 32 10.6, 1,024 15.3; 60: 256 in 21 parts 15.0 / 1,024 16.5, 128: 1,024 16.7 / in 16 parts 19.6
+// (between 60 rows and 128 neither side is measured)
 struct Split { uint32_t team, parts, chunks; bool few; };   // few: a compute unit has one workgroup at most, which may use twice the registers
 Split split_of(const vl_token_rows *a, uint32_t n_top, bool lead) {
   const uint32_t n = chunks_of(a, lead), rows = a->n_row;
